@@ -291,7 +291,7 @@ def _plain_append(s):
         parts, stands = [s["latent"].view(torch.uint8)], x
     elif form == "fp8":
         t = x.view(n, T, 4, 128)
-        scale = (t.abs().amax(3) / FP8_MOST).clamp(min=FP8_TINY)
+        scale = (t.abs().amax(3) / torch.tensor(FP8_MOST, device=x.device)).clamp(min=FP8_TINY)       # (by a number: times its reciprocal)
         code = (t / scale[..., None]).clamp(-FP8_MOST, FP8_MOST).to(torch.float8_e4m3fn)
         parts = [code.view(n, T, 512).view(torch.uint8), scale.view(torch.uint8)]
         stands = code.float() * scale[..., None]
@@ -423,7 +423,7 @@ def _exact_append(s):
         out, stands = [placed(0, torch.cat((x, turned), -1))], x
     elif c["form"] == "fp8":
         t = x.view(n, T, 4, 128)
-        scale = (t.abs().amax(3).float() / FP8_MOST).clamp(min=FP8_TINY).double()
+        scale = (t.abs().amax(3) / FP8_MOST).float().clamp(min=FP8_TINY).double()
         v = _nearest64(t / scale[..., None], 3, -6).clamp(-448, 448)
         out = [placed(0, v.view(n, T, 512)), placed(1, scale), placed(2, turned)]
         stands = (v * scale[..., None]).view(n, T, 512)
