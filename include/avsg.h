@@ -467,6 +467,125 @@ int avsg_step_noalloc(const avsg_noalloc_args *args, void *cuda_stream);
 int avsg_host_kv_alloc(size_t bytes, uint32_t flags, void **out, uint64_t *huge_bytes);
 int avsg_host_kv_free(void *base);
 
+/*
+ * Rows with a known inside (the paper moves rows without looking into them: 1152 bytes of (64 + 512) x bf16 in App. D).
+ * What one position of a layer leaves in the cache of latent attention: a latent of AVSG_LATENT_DIMS numbers, keys and values
+ * at once, and AVSG_ROPE_DIMS numbers of the key that carry the position's rotation.  Rows begin on 16-byte boundaries.
+ */
+#define AVSG_LATENT_DIMS 512u
+#define AVSG_ROPE_DIMS    64u
+#define AVSG_ROW_BF16 0u   /* 1152 bytes: 512 bf16, 64 bf16                                                       */
+#define AVSG_ROW_FP8  1u   /*  656 bytes: 512 e4m3; 4 fp32 scales, one for 128 numbers; 64 bf16                   */
+#define AVSG_ROW_FP4  2u   /*  400 bytes: 512 e2m1, two to a byte, the one with the even number in the low half;
+                              16 e8m0 scales (2 to the power of the byte - 127; 255: not a number), one for
+                              32 numbers; 64 bf16                                                                 */
+/* Bytes of a row of that format; 0 for any other number. */
+uint32_t avsg_row_bytes(uint32_t row_format);
+
+/* Rotation of the AVSG_ROPE_DIMS numbers by their position p: pair i turns by the angle p * inv_freq[i], and is multiplied by
+ * scale.  Pair i is the numbers (2 i, 2 i + 1), or (i, i + 32) with halves != 0.  Angles are formed in 64 bits. */
+typedef struct {
+    double   inv_freq[32];
+    float    scale;
+    uint32_t halves;
+} avsg_rope;
+
+/*
+ * avsg_append - writes the rows of new positions into their cache, from which avsg_step fetches them.
+ * (Sec. 3.1 has the full KV history in host memory; how it gets there is not in the paper.)
+ *
+ * For every table i and token t: the latent goes into the row in the row's format, the rotated numbers behind it as bf16.
+ *   AVSG_ROW_BF16  the latent as it is (fp16 and fp32 latents are rounded to bf16)
+ *   AVSG_ROW_FP8   per 128 numbers: scale = max(largest magnitude / 448, 2^-126) rounded to fp32; number / scale to the
+ *                  nearest e4m3, ties to even.  A group with an infinity or a NaN reads as NaN
+ *   AVSG_ROW_FP4   per 32 numbers: scale = 2^(floor(log2(largest magnitude)) - 2), at least 2^-127 (and that for a group of
+ *                  zeros); number / scale to the nearest e2m1, ties to even, beyond 6 to 6.  A group with an infinity or a
+ *                  NaN gets the scale 255
+ * (magnitudes below 2^-126 count as zero).  Rows that no token of the call names are left as they are.
+ *
+ * ctx may be NULL.  With a context, table_ids names its tables, problems go to the context's status word, and
+ * row_format has to be of the context's row_bytes.  Without one table_ids is
+ * NULL, the call runs on the device that `positions` lies on, and problems go to *status.
+ * Asynchronous on cuda_stream; host arrays are consumed before the call returns.  Two tokens of one call must not name the
+ * same row: its bytes would be some of one and some of the other.
+ */
+#define AVSG_TYPE_BF16 0u
+#define AVSG_TYPE_FP16 1u
+#define AVSG_TYPE_FP32 2u
+typedef struct {
+    uint32_t        n;              /* tables, at most 2048                                                 */
+    uint32_t        n_tokens;       /* new positions per table                                              */
+    uint32_t        row_format;     /* AVSG_ROW_*                                                           */
+    uint32_t        type;           /* AVSG_TYPE_* of latent and rope_part                                  */
+    const uint32_t *table_ids;      /* HOST [n], distinct, with a context; NULL without                     */
+    const void     *latent;         /* DEVICE [n][n_tokens][512]                                            */
+    const void     *rope_part;      /* DEVICE [n][n_tokens][64], before its rotation                        */
+    uint64_t        latent_stride[2];  /* bytes between tables, tokens; multiples of 16                     */
+    uint64_t        rope_stride[2];    /* (so may latent and rope_part be parts of one projection)          */
+    const int32_t  *positions;      /* DEVICE [n][n_tokens]; negative: no token (padding)                   */
+    const int32_t  *rows;           /* DEVICE [n][n_tokens] or NULL: the row that a token goes to, where that
+                                       is not its position (a cache in pages); negative: not written        */
+    const void *const *kv_base;     /* HOST [n]: row 0 of each table's cache, pinned host or device memory.  NULL: tables
+                                       lie one behind another in ONE allocation, see kv                     */
+    void           *kv;             /* kv_base == NULL: row 0 of table 0                                    */
+    uint64_t        kv_table_stride;   /* kv_base == NULL: bytes between tables, a multiple of 16           */
+    const uint64_t *row_stride;     /* HOST [n] or NULL (= bytes of a row): bytes between rows, multiples of 16 */
+    const uint32_t *kv_rows;        /* HOST [n] or NULL: rows of each cache; a token beyond them is not written and
+                                       reported as AVSG_STATUS_BAD_ID                                       */
+    const avsg_rope *rope;          /* HOST, or NULL: rope_part comes rotated                               */
+    void           *values;         /* DEVICE out bf16 [n][n_tokens][576] or NULL: the numbers that the rows stand for, rounded
+                                       to bf16: what attention among the new positions reads so that it sees what later
+                                       reads of the cache will.  Not written for tokens without a row       */
+    uint32_t       *status;         /* DEVICE in/out or NULL: AVSG_STATUS_* bits are added (without a context) */
+} avsg_append_args;
+
+int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
+
+/*
+ * avsg_attend - the sparse attention that reads the rows through the slot table of avsg_step (Sec. 3.1: attention reads
+ * buffer[O]).  Latent attention in its absorbed form: `heads` queries of 576 numbers share a table's rows; row k's key is its
+ * 512 latent and 64 rotated numbers, its value the latent.  For table i, token t, head h over the K positions of slots[i][t]:
+ *   s_k = scale * (q . key_k),  then softcap * tanh(s_k / softcap) if softcap > 0,  then + slopes[h] * (ids_k - position)
+ *   out = sum_k exp(s_k - lse) * value_k,      lse = log(sum_k exp(s_k))
+ * over the positions with a slot >= 0 and, where spans are given, spans[0] <= id < spans[1] (what a query may see: the end
+ * alone makes a causal mask, both a document's, an end beyond its own position a prefix's).  A query that sees nothing gets
+ * out = 0 and lse = -infinity.  Masked positions are not read, whatever their rows hold; a slot >= the rows of a table is
+ * masked too and reported as AVSG_STATUS_BAD_SLOT.
+ *
+ * ctx may be NULL.  With a context, rows are read from its buffers (buffer NULL), table_ids names the tables, which may repeat, and
+ * row_format has to be of the context's row_bytes.  Without one table_ids is NULL and buffer holds n tables of buffer_slots rows
+ * (avsg_step_noalloc's layout); the call runs on the device that `slots` lies on.  Asynchronous on cuda_stream, nothing is allocated
+ * and no state is kept: calls may overlap one another.
+ */
+typedef struct {
+    uint32_t        n;              /* tables, at most 2048                                                 */
+    uint32_t        n_tokens, topk; /* as in the avsg_step call that filled slots                           */
+    uint32_t        heads;          /* 1 .. 1024                                                            */
+    uint32_t        row_format;     /* AVSG_ROW_*                                                           */
+    uint32_t        buffer_slots;   /* rows per table, without a context                                    */
+    uint64_t        buffer_row_bytes; /* bytes between rows, without a context; 0 = bytes of a row          */
+    const uint32_t *table_ids;      /* HOST [n] with a context; NULL without                                */
+    const void     *buffer;         /* DEVICE [n][buffer_slots] rows without a context; NULL with one       */
+    const int32_t  *slots;          /* DEVICE [n][n_tokens][topk]                                           */
+    const void     *q;              /* DEVICE bf16 [n][n_tokens][heads][576]                                */
+    uint64_t        q_stride[3];    /* bytes between tables, tokens, heads; multiples of 16                 */
+    void           *out;            /* DEVICE out bf16 [n][n_tokens][heads][512]                            */
+    uint64_t        out_stride[3];  /* bytes between tables, tokens, heads; multiples of 16                 */
+    float          *lse;            /* DEVICE out [n][n_tokens][heads], natural logarithm, or NULL          */
+    float           scale;          /* finite                                                               */
+    float           softcap;        /* > 0, or 0: none                                                      */
+    const int32_t  *ids;            /* DEVICE [n][n_tokens][topk]: the positions that the slots hold (indices of
+                                       avsg_step); NULL unless spans or slopes are given                    */
+    const int32_t  *positions;      /* DEVICE [n][n_tokens]: the queries' positions; NULL unless slopes or rope are given */
+    const int32_t  *spans;          /* DEVICE [n][n_tokens][2] or NULL                                      */
+    const float    *slopes;         /* DEVICE [heads] or NULL                                               */
+    const avsg_rope *rope;          /* HOST, or NULL: the last 64 numbers of q come rotated; else they are rotated by
+                                       `positions` and rounded to bf16 again                                */
+    uint32_t       *status;         /* DEVICE in/out or NULL: AVSG_STATUS_* bits are added (without a context) */
+} avsg_attend_args;
+
+int avsg_attend(avsg_ctx *ctx, const avsg_attend_args *args, void *cuda_stream);
+
 /* No passage of the paper: a static string naming an AVSG_E* code. */
 const char *avsg_strerror(int code);
 

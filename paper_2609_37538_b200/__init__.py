@@ -6,4 +6,5 @@ from .binding import (  # noqa: F401
     AvsgConfig, AvsgError, AvsgStats, AvsgStepArgs, Context, PreparedCall, StepOutput,
     load_library, pinned_empty, HostKV, HOST_KV_HUGE_PAGES,
     AvsgNoAllocArgs, NOALLOC_MAX_IDS, NOALLOC_MAX_TABLES, step_noalloc,
+    AvsgAppendArgs, AvsgAttendArgs, AvsgRope, LATENT_DIMS, ROPE_DIMS, ROW_BF16, ROW_FP4, ROW_FP8, Rope, append, attend, row_bytes,
 )

@@ -22,6 +22,8 @@ from . import build as _build
 OK, EINVAL, ENOMEM, ECUDA, ECAPACITY, EDEVICE_STATUS, EUNSUPPORTED = 0, -1, -2, -3, -4, -5, -6
 XFER_SM_BALANCED, XFER_COPY_ENGINE, XFER_REQUEST_LEVEL, XFER_ALL_K, XFER_POSITION_LEVEL, XFER_SM_OVERLAP = 0, 1, 2, 3, 4, 5
 INDEX_HASH, INDEX_DIRECT, INDEX_PAPER = 0, 1, 2
+ROW_BF16, ROW_FP8, ROW_FP4 = 0, 1, 2
+LATENT_DIMS, ROPE_DIMS = 512, 64
 STATUS_PROBE_EXHAUSTED, STATUS_NO_DEAD_SLOTS, STATUS_BAD_SLOT, STATUS_BAD_SEGMENT, STATUS_BAD_ID, STATUS_WAIT_TIMEOUT = (
     1, 2, 4, 8, 16, 32)
 STATUS_LAUNCH_FAILED = 64
@@ -31,7 +33,7 @@ EXPORTS = (
     "avsg_sync_status", "avsg_export_state", "avsg_import_state", "avsg_save_state", "avsg_restore_state",
     "avsg_set_transfer_mode", "avsg_set_timing", "avsg_set_transfer_geometry", "avsg_strerror",
     "avsg_step_noalloc", "avsg_export_hash_state", "avsg_import_hash_state", "avsg_clear_status",
-    "avsg_probe_wait_limit", "avsg_host_kv_alloc", "avsg_host_kv_free",
+    "avsg_probe_wait_limit", "avsg_host_kv_alloc", "avsg_host_kv_free", "avsg_row_bytes", "avsg_append", "avsg_attend",
 )
 
 
@@ -70,6 +72,28 @@ class AvsgNoAllocArgs(ctypes.Structure):
                 ("indices", ctypes.c_void_p), ("kv_base", ctypes.c_void_p), ("row_stride", ctypes.c_void_p),
                 ("verified_len", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("hit", ctypes.c_void_p),
                 ("miss_count", ctypes.c_void_p), ("status", ctypes.c_void_p), ("kv_rows", ctypes.c_void_p)]
+
+
+class AvsgRope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_double * 32), ("scale", ctypes.c_float), ("halves", ctypes.c_uint32)]
+
+
+class AvsgAppendArgs(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_uint32), ("n_tokens", ctypes.c_uint32), ("row_format", ctypes.c_uint32), ("type", ctypes.c_uint32),
+                ("table_ids", ctypes.c_void_p), ("latent", ctypes.c_void_p), ("rope_part", ctypes.c_void_p),
+                ("latent_stride", ctypes.c_uint64 * 2), ("rope_stride", ctypes.c_uint64 * 2), ("positions", ctypes.c_void_p),
+                ("rows", ctypes.c_void_p), ("kv_base", ctypes.c_void_p), ("kv", ctypes.c_void_p), ("kv_table_stride", ctypes.c_uint64),
+                ("row_stride", ctypes.c_void_p), ("kv_rows", ctypes.c_void_p), ("rope", ctypes.c_void_p), ("values", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
+
+
+class AvsgAttendArgs(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_uint32), ("n_tokens", ctypes.c_uint32), ("topk", ctypes.c_uint32), ("heads", ctypes.c_uint32),
+                ("row_format", ctypes.c_uint32), ("buffer_slots", ctypes.c_uint32), ("buffer_row_bytes", ctypes.c_uint64),
+                ("table_ids", ctypes.c_void_p), ("buffer", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("q", ctypes.c_void_p),
+                ("q_stride", ctypes.c_uint64 * 3), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_uint64 * 3), ("lse", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("ids", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("spans", ctypes.c_void_p), ("slopes", ctypes.c_void_p), ("rope", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
 NOALLOC_MAX_TABLES, NOALLOC_MAX_IDS = 32, 131072
@@ -135,6 +159,9 @@ def load_library():
     lib.avsg_host_kv_alloc.argtypes = [ctypes.c_size_t, u32, ctypes.POINTER(vp), ctypes.POINTER(ctypes.c_uint64)]
     lib.avsg_host_kv_alloc.restype = i32
     lib.avsg_host_kv_free.argtypes, lib.avsg_host_kv_free.restype = [vp], i32
+    lib.avsg_row_bytes.argtypes, lib.avsg_row_bytes.restype = [u32], u32
+    lib.avsg_append.argtypes, lib.avsg_append.restype = [vp, ctypes.POINTER(AvsgAppendArgs), vp], i32
+    lib.avsg_attend.argtypes, lib.avsg_attend.restype = [vp, ctypes.POINTER(AvsgAttendArgs), vp], i32
     _lib = lib
     return lib
 
@@ -383,6 +410,15 @@ class Context:
         call.run(indices, verified_len, slots, hit, mc, stream, host=True)
         return StepOutput(slots, hit, mc)
 
+    # -- rows into the cache, attention over the buffer -------------------------------------------------
+    def append(self, table_ids, latent, rope_part, positions, kv, *, row_format: int, **kw):
+        """append() into the caches of this context's tables; problems go to its status word (sync_status)."""
+        return append(latent, rope_part, positions, kv, row_format=row_format, _ctx=self, _tables=table_ids, **kw)
+
+    def attend(self, table_ids, q, slots, *, row_format: int, scale: float, **kw):
+        """attend() over the buffers of these tables, slots as step() filled them (in the same order of tables)."""
+        return attend(q, None, slots, row_format=row_format, scale=scale, _ctx=self, _tables=table_ids, **kw)
+
     # -- state ----------------------------------------------------------------------------------------
     def reset(self, table_ids: Sequence[int]) -> None:
         ids = (ctypes.c_uint32 * len(table_ids))(*[int(t) for t in table_ids])
@@ -532,3 +568,164 @@ def step_noalloc(tok, life, buffer, indices, kv, verified_len, *, max_lifetime: 
         rc = _NOALLOC(_noalloc_fn)(ctypes.addressof(a), _stream_handle(stream))
     if rc != OK:
         _check(rc, "avsg_step_noalloc")
+
+
+def row_bytes(row_format: int) -> int:
+    """Bytes of a row of that format: 1152, 656, 400."""
+    n = load_library().avsg_row_bytes(row_format)
+    if not n:
+        raise AvsgError(EINVAL, "row_bytes: no such row format: %r" % (row_format,))
+    return n
+
+
+class Rope:
+    """Rotation of the last 64 numbers by their position: pair i by the angle position * inv_freq[i], times scale; pairs are
+    neighbours, or (halves) 32 apart."""
+
+    def __init__(self, inv_freq: Sequence[float], scale: float = 1.0, halves: bool = False):
+        inv_freq = [float(f) for f in inv_freq]
+        if len(inv_freq) != ROPE_DIMS // 2:
+            raise AvsgError(EINVAL, "Rope: inv_freq holds %d numbers, not %d" % (len(inv_freq), ROPE_DIMS // 2))
+        self.c = AvsgRope((ctypes.c_double * 32)(*inv_freq), float(scale), int(bool(halves)))
+
+
+def _need(ok, what: str) -> None:
+    if not ok:
+        raise AvsgError(EINVAL, what)
+
+
+def _device_tensor(x, name: str, dtype, shape, device):
+    """Address of a contiguous device tensor of that type and shape."""
+    _need(x.dtype == dtype and tuple(x.shape) == tuple(shape) and x.device == device and x.is_contiguous(),
+          "%s: expected a contiguous %s tensor %s on %s, got %s %s on %s" % (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr()
+
+
+def _stream_of(stream, device):
+    """Handle of the stream of a call whose tensors lie on `device`: by default that device's current one."""
+    if stream is not None:
+        return _stream_handle(stream)
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return (raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream) or None
+
+
+def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[Rope] = None, rows=None, row_stride=None, kv_rows=None,
+           want_values: bool = False, values=None, status=None, stream=None, _ctx=None, _tables=None):
+    """avsg_append: the rows of new positions, rotated and quantised on their way into the cache.
+
+    latent [n, n_tokens, 512] and rope_part [n, n_tokens, 64]: CUDA tensors of one type (bf16, fp16, fp32), parts of a wider
+    projection too; positions int32 [n, n_tokens], negative = padding; rows int32 like positions: where a token's row goes, if
+    not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
+    table, as avsg_step takes them; a tensor [rows, bytes] is a pool that all tables share.  Returns the values tensor (bf16 [n,
+    n_tokens, 576], what the rows stand for) where one is wanted, else None."""
+    import torch
+    a = AvsgAppendArgs()
+    device = latent.device
+    _need(latent.is_cuda and latent.dim() == 3 and latent.shape[2] == LATENT_DIMS, "append: latent is a CUDA tensor [n, n_tokens, 512]")
+    n, n_tokens = latent.shape[0], latent.shape[1]
+    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    _need(latent.dtype in kinds and rope_part.dtype == latent.dtype and rope_part.device == device and
+          tuple(rope_part.shape) == (n, n_tokens, ROPE_DIMS) and latent.stride(2) == 1 and rope_part.stride(2) == 1,
+          "append: rope_part is a tensor [n, n_tokens, 64] of latent's type and device, both with their last numbers side by side")
+    size = latent.element_size()
+    a.n, a.n_tokens, a.row_format, a.type = n, n_tokens, row_format, kinds[latent.dtype]
+    a.latent, a.rope_part = latent.data_ptr(), rope_part.data_ptr()
+    # (a dimension of one may have any stride)
+    for to, x in ((a.latent_stride, latent), (a.rope_stride, rope_part)):
+        to[0] = x.stride(0) * size if n > 1 else 0
+        to[1] = x.stride(1) * size if n_tokens > 1 else 0
+    a.positions = _device_tensor(positions, "append: positions", torch.int32, (n, n_tokens), device)
+    if rows is not None:
+        a.rows = _device_tensor(rows, "append: rows", torch.int32, (n, n_tokens), device)
+    keep = []
+    if hasattr(kv, "data_ptr") and not isinstance(kv, (list, tuple)):
+        _need(kv.dtype == torch.uint8 and kv.dim() in (2, 3) and kv.stride(-1) == 1 and kv.shape[-1] == row_bytes(row_format) and
+              (kv.dim() == 2 or kv.shape[0] == n) and (kv.device == device or not kv.is_cuda),
+              "append: kv is a uint8 tensor [n, rows, row bytes] or [rows, row bytes] on latent's device or pinned, or a list of caches")
+        _need(row_stride is None, "append: row_stride goes with a list of caches")
+        a.kv, a.kv_table_stride = kv.data_ptr(), (kv.stride(0) if kv.dim() == 3 and n > 1 else 0)
+        if kv_rows is None:
+            kv_rows = [kv.shape[-2]] * n
+        if kv.shape[-2] > 1 and kv.stride(-2) != kv.shape[-1]:
+            row_stride = [kv.stride(-2)] * n
+    else:
+        kv = list(kv)
+        _need(len(kv) == n, "append: one cache per table")
+        owner, a.kv_base = _c_array("Q", [_addr(k) for k in kv], n)
+        keep.append(owner)
+    for name, kind, given in (("row_stride", "Q", row_stride), ("kv_rows", "I", kv_rows), ("table_ids", "I", _tables)):
+        owner, at = _c_array(kind, given, n)
+        keep.append(owner)
+        setattr(a, name, at)
+    if rope is not None:
+        a.rope = ctypes.addressof(rope.c)
+    if want_values and values is None:
+        values = torch.empty((n, n_tokens, LATENT_DIMS + ROPE_DIMS), dtype=torch.bfloat16, device=device)
+    if values is not None:
+        a.values = _device_tensor(values, "append: values", torch.bfloat16, (n, n_tokens, LATENT_DIMS + ROPE_DIMS), device)
+    if status is not None:
+        a.status = _addr(status)
+    rc = load_library().avsg_append(_ctx._h if _ctx is not None else None, ctypes.byref(a), _stream_of(stream, device))
+    if rc != OK:
+        _check(rc, "avsg_append")
+    return values
+
+
+def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=None, want_lse: bool = False, softcap: float = 0.0, ids=None,
+           positions=None, spans=None, slopes=None, rope: Optional[Rope] = None, status=None, stream=None, _ctx=None, _tables=None):
+    """avsg_attend: the sparse attention that reads the rows of `buffer` through the slot table of avsg_step.
+
+    q: bf16 CUDA tensor [n, n_tokens, heads, 576]; buffer: uint8 [n, slots per table, row bytes] (avsg_step_noalloc's state;
+    Context.attend reads the context's own); slots int32 [n, n_tokens, topk], negative = padding.  Optional: softcap; ids int32
+    like slots with spans int32 [n, n_tokens, 2] (the ids [begin, end) that a query may see) and slopes fp32 [heads] with positions
+    int32 [n, n_tokens] (a bias of slope * (id - position)); rope with positions: q's last 64 numbers are rotated here.
+    Returns bf16 [n, n_tokens, heads, 512], and with want_lse the fp32 logarithms [n, n_tokens, heads] too."""
+    import torch
+    a = AvsgAttendArgs()
+    device = q.device
+    _need(q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 4 and q.shape[3] == LATENT_DIMS + ROPE_DIMS and q.stride(3) == 1,
+          "attend: q is a bf16 CUDA tensor [n, n_tokens, heads, 576] with its last numbers side by side")
+    n, n_tokens, heads, _ = q.shape
+    _need(slots.dim() == 3, "attend: slots is [n, n_tokens, topk]")
+    topk = slots.shape[2]
+    a.n, a.n_tokens, a.topk, a.heads, a.row_format = n, n_tokens, topk, heads, row_format
+    a.slots = _device_tensor(slots, "attend: slots", torch.int32, (n, n_tokens, topk), device)
+    if _ctx is None:
+        _need(buffer.is_cuda and buffer.device == device and buffer.dtype == torch.uint8 and buffer.dim() == 3 and buffer.shape[0] == n and
+              buffer.stride(2) == 1 and buffer.shape[2] == row_bytes(row_format) and
+              (n == 1 or buffer.stride(0) == buffer.stride(1) * buffer.shape[1]),
+              "attend: buffer is a uint8 tensor [n, slots, row bytes] on q's device, its tables one behind another")
+        a.buffer, a.buffer_slots, a.buffer_row_bytes = buffer.data_ptr(), buffer.shape[1], (buffer.stride(1) if buffer.shape[1] > 1 else 0)
+    else:
+        _need(len(_tables) == n, "attend: one table per query block")
+        owner, a.table_ids = _c_array("I", _tables, n)
+    if out is None:
+        out = torch.empty((n, n_tokens, heads, LATENT_DIMS), dtype=torch.bfloat16, device=device)
+    _need(out.dtype == torch.bfloat16 and out.device == device and tuple(out.shape) == (n, n_tokens, heads, LATENT_DIMS) and out.stride(3) == 1,
+          "attend: out is a bf16 tensor [n, n_tokens, heads, 512] on q's device with its last numbers side by side")
+    a.q, a.out = q.data_ptr(), out.data_ptr()
+    for to, x in ((a.q_stride, q), (a.out_stride, out)):
+        for i in range(3):
+            to[i] = 2 * x.stride(i) if x.shape[i] > 1 else 0
+    if want_lse and lse is None:
+        lse = torch.empty((n, n_tokens, heads), dtype=torch.float32, device=device)
+    if lse is not None:
+        a.lse = _device_tensor(lse, "attend: lse", torch.float32, (n, n_tokens, heads), device)
+    a.scale, a.softcap = scale, softcap
+    if ids is not None:
+        a.ids = _device_tensor(ids, "attend: ids", torch.int32, (n, n_tokens, topk), device)
+    if positions is not None:
+        a.positions = _device_tensor(positions, "attend: positions", torch.int32, (n, n_tokens), device)
+    if spans is not None:
+        a.spans = _device_tensor(spans, "attend: spans", torch.int32, (n, n_tokens, 2), device)
+    if slopes is not None:
+        a.slopes = _device_tensor(slopes, "attend: slopes", torch.float32, (heads,), device)
+    if rope is not None:
+        a.rope = ctypes.addressof(rope.c)
+    if status is not None:
+        a.status = _addr(status)
+    rc = load_library().avsg_attend(_ctx._h if _ctx is not None else None, ctypes.byref(a), _stream_of(stream, device))
+    if rc != OK:
+        _check(rc, "avsg_attend")
+    return (out, lse) if lse is not None else out

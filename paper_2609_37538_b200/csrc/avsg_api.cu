@@ -10,6 +10,7 @@
 #include "avsg.h"
 #include "avsg_kernels.cuh"
 #include "host_buffers.h"
+#include "rows.h"
 
 using namespace avsg;
 
@@ -143,6 +144,18 @@ int resolve_kv(avsg_ctx* c, uint32_t table, const void* host_ptr, uint64_t* dev)
     return AVSG_OK;
 }
 
+// Every table of a call exists and comes once.
+int distinct_tables(avsg_ctx* c, const uint32_t* table_ids, uint32_t n)
+{
+    if (++c->epoch == 0) { std::fill(c->seen.begin(), c->seen.end(), 0u); c->epoch = 1; }
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint32_t t = table_ids[i];
+        if (t >= c->cfg.num_tables || c->seen[t] == c->epoch) return AVSG_EINVAL;
+        c->seen[t] = c->epoch;
+    }
+    return AVSG_OK;
+}
+
 int check_args(avsg_ctx* c, const avsg_step_args* a)
 {
     if (!c || !a) return AVSG_EINVAL;
@@ -152,11 +165,9 @@ int check_args(avsg_ctx* c, const avsg_step_args* a)
     if (a->n_tokens == 0 || a->n_tokens > c->cfg.max_tokens || a->topk == 0 || a->topk > c->cfg.max_topk)
         return AVSG_EINVAL;
     if ((uint64_t)a->n_tokens * a->topk > c->cfg.buffer_slots) return AVSG_ECAPACITY;      // Eq. 7
-    if (++c->epoch == 0) { std::fill(c->seen.begin(), c->seen.end(), 0u); c->epoch = 1; }
+    const int rc = distinct_tables(c, a->table_ids, a->n);
+    if (rc != AVSG_OK) return rc;
     for (uint32_t i = 0; i < a->n; ++i) {
-        const uint32_t t = a->table_ids[i];
-        if (t >= c->cfg.num_tables || c->seen[t] == c->epoch) return AVSG_EINVAL;
-        c->seen[t] = c->epoch;
         if (a->row_stride && (a->row_stride[i] % 16 || a->row_stride[i] < c->cfg.row_bytes)) return AVSG_EINVAL;
         if (!a->kv_base[i] || (reinterpret_cast<uint64_t>(a->kv_base[i]) & 15u)) return AVSG_EINVAL;
         if (a->kv_rows && a->kv_rows[i] > 0x80000000u) return AVSG_EINVAL;
@@ -576,7 +587,8 @@ int avsg_create(const avsg_config* cfg, avsg_ctx** out)
     // always raise the kernels' dynamic shared-memory limit to the device maximum: the attribute is
     // per function, so a context with a small table must not lower it under a context with a large one
     if (stage_one_prepare((size_t)max_smem) != cudaSuccess || step_prepare((size_t)max_smem) != cudaSuccess || stage_one_cluster_prepare((size_t)max_smem) != cudaSuccess ||
-        transfer_prepare() != cudaSuccess || arriving_prepare() != cudaSuccess) {
+        transfer_prepare() != cudaSuccess || arriving_prepare() != cudaSuccess || append_prepare() != cudaSuccess ||
+        attend_prepare() != cudaSuccess) {
         delete c; return AVSG_ECUDA;
     }
     c->step_clusters = step_clusters((size_t)max_smem);
@@ -708,6 +720,33 @@ int avsg_step(avsg_ctx* c, const avsg_step_args* a, void* stream)
 int avsg_step_host(avsg_ctx* c, const avsg_step_args* a, void* stream)
 {
     return step_impl(c, a, static_cast<cudaStream_t>(stream), true);
+}
+
+int avsg_append(avsg_ctx* c, const avsg_append_args* a, void* cuda_stream)
+{
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!c) return append_bare(a, stream);
+    int rc = check_append(a);
+    if (rc != AVSG_OK) return rc;
+    if (!a->table_ids || a->status || a->n > c->cfg.num_tables || row_bytes_of(a->row_format) != c->cfg.row_bytes) return AVSG_EINVAL;
+    if ((rc = distinct_tables(c, a->table_ids, a->n)) != AVSG_OK) return rc;
+    DeviceGuard guard(c->cfg.device);
+    if (!guard.ok) return AVSG_ECUDA;
+    return append_run(a, c->d_status, stream);
+}
+
+int avsg_attend(avsg_ctx* c, const avsg_attend_args* a, void* cuda_stream)
+{
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!c) return attend_bare(a, stream);
+    const int rc = check_attend(a);
+    if (rc != AVSG_OK) return rc;
+    if (!a->table_ids || a->buffer || a->buffer_slots || a->buffer_row_bytes || a->status || row_bytes_of(a->row_format) != c->cfg.row_bytes)
+        return AVSG_EINVAL;
+    for (uint32_t i = 0; i < a->n; ++i) if (a->table_ids[i] >= c->cfg.num_tables) return AVSG_EINVAL;
+    DeviceGuard guard(c->cfg.device);
+    if (!guard.ok) return AVSG_ECUDA;
+    return attend_run(a, c->d_buffer, c->cfg.buffer_slots, c->cfg.row_bytes, c->d_status, stream);
 }
 
 int avsg_buffer(avsg_ctx* c, uint32_t table_id, void** d_rows)
