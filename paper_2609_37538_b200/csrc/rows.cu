@@ -131,30 +131,27 @@ int check_attend(const avsg_attend_args* a)
 
 int attend_run(const avsg_attend_args* a, const void* buffer, uint32_t rows, uint64_t row_stride, uint32_t* status, cudaStream_t stream)
 {
-    auto fill = [&](auto& p) {
-        p.buffer = static_cast<const uint8_t*>(buffer);
-        p.table_stride = (uint64_t)rows * row_stride; p.row_stride = (uint32_t)row_stride; p.rows = rows;
-        p.slots = a->slots; p.ids = a->ids; p.positions = a->positions; p.spans = a->spans; p.slopes = a->slopes;
-        p.q = static_cast<const uint8_t*>(a->q); p.out = static_cast<uint8_t*>(a->out);
-        for (int i = 0; i < 3; ++i) { p.q_stride[i] = a->q_stride[i]; p.out_stride[i] = a->out_stride[i]; }
-        p.lse = a->lse; p.status = status;
-        p.scale = a->scale; p.softcap = a->softcap;
-        p.n = a->n; p.n_tokens = a->n_tokens; p.topk = a->topk; p.heads = a->heads;
-        p.rope = rope_params(a->rope);
-        p.mapped = a->table_ids != nullptr;
-        if (a->table_ids) memcpy(p.table_id, a->table_ids, a->n * sizeof(uint32_t));
-    };
-    cudaError_t e;
-    if (!a->table_ids || a->n <= sizeof(AttendParams::table_id) / sizeof(uint32_t)) {
-        AttendParams p;
-        fill(p);
-        e = launch_attend(p, a->row_format, stream);
-    } else {
-        AttendParamsBig p;
-        fill(p);
-        e = launch_attend(p, a->row_format, stream);
+    AttendParams p;
+    p.table_stride = (uint64_t)rows * row_stride; p.row_stride = (uint32_t)row_stride; p.rows = rows;
+    p.slopes = a->slopes; p.status = status;
+    for (int i = 0; i < 3; ++i) { p.q_stride[i] = a->q_stride[i]; p.out_stride[i] = a->out_stride[i]; }
+    p.scale = a->scale; p.softcap = a->softcap;
+    p.n_tokens = a->n_tokens; p.topk = a->topk; p.heads = a->heads;
+    p.rope = rope_params(a->rope);
+    p.mapped = a->table_ids != nullptr;
+    // Tables of a context travel as kernel arguments, as many as these hold to a launch; others need no list.
+    const uint32_t most = a->table_ids ? (uint32_t)ATTEND_MAX_TABLES : a->n;
+    for (uint32_t first = 0; first < a->n; first += most) {
+        const size_t queries = (size_t)first * a->n_tokens, ids = queries * a->topk;
+        p.n = a->n - first < most ? a->n - first : most;
+        p.buffer = static_cast<const uint8_t*>(buffer);                                     // (first > 0: tables by their ids)
+        p.slots = a->slots + ids; p.ids = a->ids ? a->ids + ids : nullptr;
+        p.positions = a->positions ? a->positions + queries : nullptr; p.spans = a->spans ? a->spans + 2 * queries : nullptr;
+        p.q = static_cast<const uint8_t*>(a->q) + first * a->q_stride[0]; p.out = static_cast<uint8_t*>(a->out) + first * a->out_stride[0];
+        p.lse = a->lse ? a->lse + queries * a->heads : nullptr;
+        if (a->table_ids) memcpy(p.table_id, a->table_ids + first, p.n * sizeof(uint32_t));
+        if (launch_attend(p, a->row_format, stream) != cudaSuccess) { cudaGetLastError(); return AVSG_ECUDA; }
     }
-    if (e != cudaSuccess) { cudaGetLastError(); return AVSG_ECUDA; }
     return AVSG_OK;
 }
 

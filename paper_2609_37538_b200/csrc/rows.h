@@ -40,8 +40,8 @@ struct AppendParams {
 cudaError_t append_prepare();
 cudaError_t launch_append(const AppendParams& p, uint32_t format, uint32_t type, cudaStream_t stream);
 
-template <int CAP>
-struct AttendParamsT {
+constexpr int ATTEND_MAX_TABLES = 128;
+struct AttendParams {
     const uint8_t* buffer;
     uint64_t table_stride; uint32_t row_stride; uint32_t rows;      // of a table
     const int32_t* slots; const int32_t* ids; const int32_t* positions; const int32_t* spans; const float* slopes;
@@ -50,15 +50,13 @@ struct AttendParamsT {
     float* lse; uint32_t* status;
     float scale, softcap;
     uint32_t n, n_tokens, topk, heads;
+    uint32_t groups, group_heads, cluster;      // set by launch_attend(): groups of heads, heads of one, blocks per query and group
     RopeParams rope;
-    uint32_t mapped;                // table_id holds the tables; else table i is i
-    uint32_t table_id[CAP];
+    uint32_t mapped;                            // table_id holds the tables; else table i is i
+    uint32_t table_id[ATTEND_MAX_TABLES];
 };
-using AttendParams = AttendParamsT<128>;
-using AttendParamsBig = AttendParamsT<ROWS_MAX_TABLES>;
 cudaError_t attend_prepare();
-cudaError_t launch_attend(const AttendParams& p, uint32_t format, cudaStream_t stream);
-cudaError_t launch_attend(const AttendParamsBig& p, uint32_t format, cudaStream_t stream);
+cudaError_t launch_attend(AttendParams& p, uint32_t format, cudaStream_t stream);
 
 // The parts of the two calls: the checks, and what follows them with a context's buffers and status word or the caller's own.
 int check_append(const avsg_append_args* a);

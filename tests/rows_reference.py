@@ -86,7 +86,7 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
     that.  Weights then are off by a factor of exp(+-2 d), rounded once to 16 bits of a float (bf16: 2^-8); values are as exact
     as keys; and the result is rounded to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the largest, results).
     Rows in 8 and 4 bits may be multiplied as fp16, in units of a power of two up to twice the row's largest scale (b): their
-    elements then are off by 2^-25 units besides, queries by 2^-37 of their largest number, and weights, held in units of which the
+    elements then are off by 2^-23 units besides, queries by 2^-37 of their largest number, and weights, held in units of which the
     largest has 2^11 or more, by 2^-25 units of the largest row's: K 2^-36 of that row's unit times its largest code."""
     n, T, H, _ = q.shape
     dev = q.device
@@ -113,7 +113,7 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             if fmt:
                 raw = buffer[i, s[at]]
                 unit = 2 * (raw[:, 512:528].contiguous().view(torch.float32).double().abs() if fmt == 1 else torch.exp2(raw[:, 256:272].double() - 127)).amax(1)
-                d = d + abs(scale) * (2.0 ** -25 * x[:, :LATENT].abs().sum(1)[:, None] * unit + 2.0 ** -37 * x[:, :LATENT].abs().amax(1)[:, None] * k[:, :LATENT].abs().sum(1))
+                d = d + abs(scale) * (2.0 ** -23 * x[:, :LATENT].abs().sum(1)[:, None] * unit + 2.0 ** -37 * x[:, :LATENT].abs().amax(1)[:, None] * k[:, :LATENT].abs().sum(1))
             if inv_freq is not None:        # a turned query that lies next to a border of bf16 may be rounded to its other side
                 d = d + (x[:, LATENT:].abs() @ k[:, LATENT:].abs().T) * abs(scale) * 2.0 ** -7 * 0.02
             if softcap:
@@ -129,7 +129,7 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             o, mass = p @ k[:, :LATENT], p @ k[:, :LATENT].abs()
             outs.append(o); lses.append(lse)
             w = 2.0 ** -8 + (2.0 ** -11 if fmt == 1 else 0.0) + torch.expm1(2 * d)[:, None]
-            less = mass * w + 2.0 ** -25 * (p @ unit)[:, None] + at.numel() * (2.0 ** -36 * unit.max() * (448.0 if fmt == 1 else 6.0) + 2.0 ** -126 * k.abs().max())
+            less = mass * w + 2.0 ** -23 * (p @ unit)[:, None] + at.numel() * (2.0 ** -36 * unit.max() * (448.0 if fmt == 1 else 6.0) + 2.0 ** -126 * k.abs().max())
             eo.append(less + (o.abs() + less) * 2.0 ** -8 + 2.0 ** -126); el.append(d + lse.abs() * 2.0 ** -22)
     back = lambda v, *tail: torch.stack(v).view(n, T, H, *tail)  # noqa: E731
     return back(outs, LATENT), back(lses), back(eo, LATENT), back(el)
