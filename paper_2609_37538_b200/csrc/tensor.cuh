@@ -22,6 +22,21 @@ __device__ __forceinline__ bool barrier_done(uint32_t bar, uint32_t parity)
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done;
 }
+// The same without a pause in it, for who looks at several barriers in turn.
+__device__ __forceinline__ bool barrier_is_done(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done;
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool one_lane()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p;
+}
 // What is written to shared memory by ordinary stores is seen by the matrix unit behind this and a barrier.
 __device__ __forceinline__ void fence_for_matrix_unit() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -41,16 +56,13 @@ __device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// 16 lanes x 64 columns of 32 bits, spread over the warp: x[4 g + i] is row lane / 4 + 8 (i / 2), column 8 g + 2 (lane % 4) + i % 2.
-__device__ __forceinline__ void tmem_load_16x64(uint32_t at, float (&x)[32])
+// 16 lanes x 32 columns of 32 bits, spread over the warp: x[4 g + i] is row lane / 4 + 8 (i / 2), column 8 g + 2 (lane % 4) + i % 2.
+__device__ __forceinline__ void tmem_load_16x32(uint32_t at, float (&x)[16])
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-                 "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(at));
 }
 // 32 lanes x 16 columns: thread i has lane i.
@@ -71,29 +83,45 @@ __device__ __forceinline__ void tmem_store_32x16(uint32_t at, const float (&x)[1
 }
 
 // ---- products ------------------------------------------------------------------------------------------------------------
-// Operands lie in shared memory in pieces of 8 x 128 bytes, 1024-byte aligned, whose 16-byte units are swizzled: unit u of line i is
-// at u ^ (i & 7).  along_k: lines are rows of the operand and run along the sum (K); else lines are steps of the sum and run along
-// rows, 64 of them, the next 64 being `next` bytes further on.  The next 8 lines are 1024 bytes further on.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t next)
+// Operands lie in shared memory in pieces of 8 lines of 128 bytes, 1024-byte aligned, whose 16-byte units are swizzled: unit u of line
+// i is at u ^ (i & 7).  Lines run along the sum, one for each row of the operand; or along rows (64 16-bit or 128 8-bit ones, the next
+// as many being `next` bytes further on), one for each step of the sum.  The next 8 lines are 1024 bytes further on.
+// An operand is its low word, to which (bytes / 16) may be added, and OPERAND_HIGH.
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t next) { return (at & 0x3FFFFu) >> 4 | (next >> 4) << 16; }
+constexpr uint32_t OPERAND_HIGH = 1024u >> 4 | 1u << 14 | 2u << 29;
+enum class Product : uint32_t { BF16 = 1u << 7 | 1u << 10, E4M3 = 0 };                // both operands' type; sums in 32 bits
+__device__ constexpr uint32_t product_shape(Product type, uint32_t m, uint32_t n, bool a_along_rows)
 {
-    return (uint64_t)((at & 0x3FFFFu) >> 4) | (uint64_t)(next >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
+    return 1u << 4 | (uint32_t)type | (a_along_rows ? 1u : 0u) << 15 | (n >> 3) << 17 | (m >> 4) << 24;
 }
-// fp16 or bf16 operands, 32-bit sums; a_along_rows: see operand().
-__device__ constexpr uint32_t product_shape(bool bf16, uint32_t m, uint32_t n, bool a_along_rows)
+// 32 bytes of lines along the sum, or 16 (bf16), 32 (e4m3) lines along rows: sums at TMEM address `to` (added to what is there if add).
+// One thread issues; see products_done().
+template <Product TYPE>
+__device__ __forceinline__ void multiply(uint32_t to, uint32_t a, uint32_t b, uint32_t shape, bool add)
 {
-    return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a_along_rows ? 1u : 0u) << 15 | (n >> 3) << 17 | (m >> 4) << 24;
-}
-// 16 steps of the sum: sums at TMEM address `to` (added to what is there if add).  One thread issues; see products_done().
-__device__ __forceinline__ void multiply(uint32_t to, uint64_t a, uint64_t b, uint32_t shape, bool add)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(to), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+    if constexpr (TYPE == Product::BF16)
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+                     :: "r"(to), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, p;\n\t}"
+                     :: "r"(to), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
 }
 // The barrier gets an arrival when all products issued by this thread so far are through.
 __device__ __forceinline__ void products_done(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
+
+// ---- copies of 16 bytes that wait in no register ---------------------------------------------------------------------------
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool zero)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(zero ? 0u : 16u) : "memory");
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int OPEN>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(OPEN) : "memory"); }
 
 // ---- clusters --------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void cluster_sync()

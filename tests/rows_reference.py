@@ -80,14 +80,14 @@ def turn(x, positions, inv_freq, scale=1.0, halves=False):
 def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, spans=None, slopes=None, inv_freq=None, rope_scale=1.0, halves=False):
     """(out, lse, bound on |out|'s error, bound on lse's error), all fp64.
 
-    The bounds: a score is a sum of 576 products of bf16 queries with keys that are exact (bf16, 4 bits) or rounded once to 11 bits
-    (e4m3 times its scale: 2^-11 of the product), added in 32 bits (576 x 2^-24 of the magnitudes' sum, doubled for the order of the
-    matrix unit's adders and its cut-off bits), then a few operations of 2^-22 each on numbers up to the largest score or cap.  d bounds
-    that.  Weights then are off by a factor of exp(+-2 d), rounded once to 16 bits of a float (bf16: 2^-8); values are as exact
-    as keys; and the result is rounded to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the largest, results).
-    Rows in 8 and 4 bits may be multiplied as fp16, in units of a power of two up to twice the row's largest scale (b): their
-    elements then are off by 2^-23 units besides, queries by 2^-37 of their largest number, and weights, held in units of which the
-    largest has 2^11 or more, by 2^-25 units of the largest row's: K 2^-36 of that row's unit times its largest code."""
+    The bounds.  A score is a sum of 576 products of bf16 queries with keys, added in 32 bits (576 x 2^-24 of the magnitudes' sum, doubled
+    for the order of the matrix unit's adders and its cut-off bits), then a few operations of 2^-22 each on numbers up to the largest
+    score or cap.  Rows in 8 and 4 bits may be multiplied as e4m3 codes times a scale for 128 numbers (4 bits: 2^-6 of the largest of the four scales), queries as
+    two e4m3 numbers: a query's elements then are off by 2^-17 of its largest one where they are below 2^-10 of it, a 4-bit row's by
+    2^-10 of that scale where they are below it.  d bounds the sum of these.  Weights then are off by a factor of exp(+-2 d) and
+    rounded to 8 bits (2^-8; in 8-bit halves after three roundings to 11 bits), and as e4m3 numbers they
+    are whole to 2^-10 / 32 of the unit of the largest row (twice its scale) where the largest weight is 1 or more.  The result is rounded
+    to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the largest, results)."""
     n, T, H, _ = q.shape
     dev = q.device
     outs, lses, eo, el = [], [], [], []
@@ -108,12 +108,18 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
                 x = torch.cat((x[:, :LATENT], turn(x[:, LATENT:], positions[i, g].expand(H), inv_freq, rope_scale, halves).to(torch.bfloat16).double()), 1)
             z = (x @ k.T) * scale
             size = (x.abs() @ k.abs().T) * abs(scale)
-            d = size * ((2.0 ** -11 if fmt == 1 else 0.0) + 2 * 576 * 2.0 ** -24)
-            unit = torch.zeros(at.numel(), dtype=torch.float64, device=dev)
+            d = size * (2 * 576 * 2.0 ** -24)
+            fine = torch.zeros((), dtype=torch.float64, device=dev).expand(at.numel(), LATENT)
             if fmt:
                 raw = buffer[i, s[at]]
-                unit = 2 * (raw[:, 512:528].contiguous().view(torch.float32).double().abs() if fmt == 1 else torch.exp2(raw[:, 256:272].double() - 127)).amax(1)
-                d = d + abs(scale) * (2.0 ** -23 * x[:, :LATENT].abs().sum(1)[:, None] * unit + 2.0 ** -37 * x[:, :LATENT].abs().amax(1)[:, None] * k[:, :LATENT].abs().sum(1))
+                unit = (raw[:, 512:528].contiguous().view(torch.float32).double().abs() if fmt == 1 else
+                        torch.exp2(raw[:, 256:272].double().view(-1, 4, 4).amax(2) - 133))
+                spread = unit.repeat_interleave(128, 1)
+                if fmt == 2:
+                    fine = spread * 2.0 ** -10 * (k[:, :LATENT].abs() < spread * 2.0 ** -5)
+                d = d + abs(scale) * (2.0 ** -17 * (x[:, :LATENT].abs().amax(1)[:, None] * (x[:, :LATENT].abs() < x[:, :LATENT].abs().amax(1)[:, None] * 2.0 ** -9)) @ k[:, :LATENT].abs().T
+                                      + x[:, :LATENT].abs() @ fine.T)
+                code = torch.where(spread > 0, k[:, :LATENT].abs() / spread, torch.zeros_like(spread))
             if inv_freq is not None:        # a turned query that lies next to a border of bf16 may be rounded to its other side
                 d = d + (x[:, LATENT:].abs() @ k[:, LATENT:].abs().T) * abs(scale) * 2.0 ** -7 * 0.02
             if softcap:
@@ -128,8 +134,10 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             p = torch.exp(z - lse[:, None])
             o, mass = p @ k[:, :LATENT], p @ k[:, :LATENT].abs()
             outs.append(o); lses.append(lse)
-            w = 2.0 ** -8 + (2.0 ** -11 if fmt == 1 else 0.0) + torch.expm1(2 * d)[:, None]
-            less = mass * w + 2.0 ** -23 * (p @ unit)[:, None] + at.numel() * (2.0 ** -36 * unit.max() * (448.0 if fmt == 1 else 6.0) + 2.0 ** -126 * k.abs().max())
+            less = mass * (2.0 ** -8 + (3 * 2.0 ** -11 if fmt else 0.0) + torch.expm1(2 * d)[:, None]) + p @ fine
+            less = less + at.numel() * 2.0 ** -126 * k.abs().max()
+            if fmt:
+                less = less + 2.0 ** -15 * 2 * unit.max() * code.sum(0) / torch.exp(lse - z.amax(1))[:, None]
             eo.append(less + (o.abs() + less) * 2.0 ** -8 + 2.0 ** -126); el.append(d + lse.abs() * 2.0 ** -22)
     back = lambda v, *tail: torch.stack(v).view(n, T, H, *tail)  # noqa: E731
     return back(outs, LATENT), back(lses), back(eo, LATENT), back(el)
