@@ -15,15 +15,16 @@ __device__ __forceinline__ void barrier_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
 }
-__device__ __forceinline__ bool barrier_done(uint32_t bar, uint32_t parity)
+// With a pause in it while the phase lasts: many warps looking all the time take shared memory's bandwidth from the matrix unit (sixteen of
+// them doubled the time of its products).
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done;
 }
-// The same without a pause in it, for who looks at several barriers in turn.
-__device__ __forceinline__ bool barrier_is_done(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool barrier_done(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -84,28 +85,29 @@ __device__ __forceinline__ void tmem_store_32x16(uint32_t at, const float (&x)[1
 
 // ---- products ------------------------------------------------------------------------------------------------------------
 // Operands lie in shared memory in pieces of 8 lines of 128 bytes, 1024-byte aligned, whose 16-byte units are swizzled: unit u of line
-// i is at u ^ (i & 7).  Lines run along the sum, one for each row of the operand; or along rows (64 16-bit or 128 8-bit ones, the next
-// as many being `next` bytes further on), one for each step of the sum.  The next 8 lines are 1024 bytes further on.
+// i is at u ^ (i & 7).  Lines run along the sum, one for each row of the operand; or along rows, 64 (16-bit ones) of them, the next 64
+// being `next` bytes further on, one for each step of the sum.  The next 8 lines are 1024 bytes further on.
 // An operand is its low word, to which (bytes / 16) may be added, and OPERAND_HIGH.
 __device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t next) { return (at & 0x3FFFFu) >> 4 | (next >> 4) << 16; }
 constexpr uint32_t OPERAND_HIGH = 1024u >> 4 | 1u << 14 | 2u << 29;
-enum class Product : uint32_t { BF16 = 1u << 7 | 1u << 10, E4M3 = 0 };                // both operands' type; sums in 32 bits
-__device__ constexpr uint32_t product_shape(Product type, uint32_t m, uint32_t n, bool a_along_rows)
+// Both operands' type; sums are in 32 bits.
+enum class Product { FP16, BF16, E4M3 };
+__host__ __device__ constexpr uint32_t product_shape(Product type, uint32_t m, uint32_t n, bool a_along_rows)
 {
-    return 1u << 4 | (uint32_t)type | (a_along_rows ? 1u : 0u) << 15 | (n >> 3) << 17 | (m >> 4) << 24;
+    return 1u << 4 | (type == Product::BF16 ? 1u << 7 | 1u << 10 : 0u) | (a_along_rows ? 1u : 0u) << 15 | (n >> 3) << 17 | (m >> 4) << 24;
 }
-// 32 bytes of lines along the sum, or 16 (bf16), 32 (e4m3) lines along rows: sums at TMEM address `to` (added to what is there if add).
-// One thread issues; see products_done().
+// 16 steps of the sum (32 for e4m3): 32 bytes of lines along it, or so many lines.  Sums at TMEM address `to`, added to what is there
+// if add.  One thread issues; see products_done().
 template <Product TYPE>
 __device__ __forceinline__ void multiply(uint32_t to, uint32_t a, uint32_t b, uint32_t shape, bool add)
 {
-    if constexpr (TYPE == Product::BF16)
+    if constexpr (TYPE == Product::E4M3)
         asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+                     "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, p;\n\t}"
                      :: "r"(to), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
     else
         asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, p;\n\t}"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
                      :: "r"(to), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add), "r"(OPERAND_HIGH) : "memory");
 }
 // The barrier gets an arrival when all products issued by this thread so far are through.

@@ -82,12 +82,13 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
 
     The bounds.  A score is a sum of 576 products of bf16 queries with keys, added in 32 bits (576 x 2^-24 of the magnitudes' sum, doubled
     for the order of the matrix unit's adders and its cut-off bits), then a few operations of 2^-22 each on numbers up to the largest
-    score or cap.  Rows in 8 and 4 bits may be multiplied as e4m3 codes times a scale for 128 numbers (4 bits: 2^-6 of the largest of the four scales), queries as
-    two e4m3 numbers: a query's elements then are off by 2^-17 of its largest one where they are below 2^-10 of it, a 4-bit row's by
-    2^-10 of that scale where they are below it.  d bounds the sum of these.  Weights then are off by a factor of exp(+-2 d) and
-    rounded to 8 bits (2^-8; in 8-bit halves after three roundings to 11 bits), and as e4m3 numbers they
-    are whole to 2^-10 / 32 of the unit of the largest row (twice its scale) where the largest weight is 1 or more.  The result is rounded
-    to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the largest, results)."""
+    score or cap.  Queries may be two e4m3 numbers, of 4 bits each: off by 2^-17 of the largest one where an element is below 2^-10 of that; or fp16
+    in units of 2^-14 of the largest number or finer (off by 2^-38 of it), with 4-bit rows in units of 2^-13 of the row's largest scale, elements
+    off by 2^-25 of these.  d bounds the sum of these.  Weights then are off by a factor of exp(+-2 d) and rounded to 16 bits (bf16: 2^-8; fp16
+    rows: three times 2^-11, the row's unit going onto them too); as fp16 they are whole to 2^-25 / 16 of the unit of the largest row (twice its
+    scale) where the largest weight is 1 or more.  Values of 8-bit rows are fp16, in units of up to 2^-6 of the row's largest scale: off by 2^-11,
+    twice (scale and product), and by 2^-25 x 448 of these units where a scale is far below the row's largest.  The result is rounded to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the
+    largest, results), and so may what is below 2^-100 in rows of 8 and 4 bits."""
     n, T, H, _ = q.shape
     dev = q.device
     outs, lses, eo, el = [], [], [], []
@@ -109,16 +110,21 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             z = (x @ k.T) * scale
             size = (x.abs() @ k.abs().T) * abs(scale)
             d = size * (2 * 576 * 2.0 ** -24)
-            fine = torch.zeros((), dtype=torch.float64, device=dev).expand(at.numel(), LATENT)
+            fine = torch.zeros(at.numel(), dtype=torch.float64, device=dev)
             if fmt:
                 raw = buffer[i, s[at]]
-                unit = (raw[:, 512:528].contiguous().view(torch.float32).double().abs() if fmt == 1 else
-                        torch.exp2(raw[:, 256:272].double().view(-1, 4, 4).amax(2) - 133))
-                spread = unit.repeat_interleave(128, 1)
-                if fmt == 2:
-                    fine = spread * 2.0 ** -10 * (k[:, :LATENT].abs() < spread * 2.0 ** -5)
-                d = d + abs(scale) * (2.0 ** -17 * (x[:, :LATENT].abs().amax(1)[:, None] * (x[:, :LATENT].abs() < x[:, :LATENT].abs().amax(1)[:, None] * 2.0 ** -9)) @ k[:, :LATENT].abs().T
-                                      + x[:, :LATENT].abs() @ fine.T)
+                if fmt == 1:
+                    unit = raw[:, 512:528].contiguous().view(torch.float32).double().abs()
+                    fine = 2.0 ** -25 * 448 * 2.0 ** -6 * unit.amax(1)
+                else:
+                    unit = torch.exp2(raw[:, 256:272].double().amax(1, keepdim=True).clamp(min=40) - 140)
+                    fine = 2.0 ** -25 * unit[:, 0]
+                spread = unit.repeat_interleave(512 // unit.shape[1], 1)
+                top = x[:, :LATENT].abs().amax(1)[:, None]
+                if fmt == 1:
+                    d = d + abs(scale) * 2.0 ** -17 * (top * (x[:, :LATENT].abs() < top * 2.0 ** -9)) @ k[:, :LATENT].abs().T
+                else:
+                    d = d + abs(scale) * (2.0 ** -38 * top * k[:, :LATENT].abs().sum(1) + x[:, :LATENT].abs().sum(1)[:, None] * fine)
                 code = torch.where(spread > 0, k[:, :LATENT].abs() / spread, torch.zeros_like(spread))
             if inv_freq is not None:        # a turned query that lies next to a border of bf16 may be rounded to its other side
                 d = d + (x[:, LATENT:].abs() @ k[:, LATENT:].abs().T) * abs(scale) * 2.0 ** -7 * 0.02
@@ -134,10 +140,10 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             p = torch.exp(z - lse[:, None])
             o, mass = p @ k[:, :LATENT], p @ k[:, :LATENT].abs()
             outs.append(o); lses.append(lse)
-            less = mass * (2.0 ** -8 + (3 * 2.0 ** -11 if fmt else 0.0) + torch.expm1(2 * d)[:, None]) + p @ fine
-            less = less + at.numel() * 2.0 ** -126 * k.abs().max()
+            less = mass * ((0.0, 5 * 2.0 ** -11, 3 * 2.0 ** -11)[fmt] + (0.0 if fmt else 2.0 ** -8) + torch.expm1(2 * d)[:, None]) + (p @ fine)[:, None]
+            less = less + at.numel() * (2.0 ** -126 * k.abs().max() + (2.0 ** -100 if fmt else 0.0))
             if fmt:
-                less = less + 2.0 ** -15 * 2 * unit.max() * code.sum(0) / torch.exp(lse - z.amax(1))[:, None]
+                less = less + 2.0 ** -29 * 2 * unit.max() * code.sum(0) / torch.exp(lse - z.amax(1))[:, None]
             eo.append(less + (o.abs() + less) * 2.0 ** -8 + 2.0 ** -126); el.append(d + lse.abs() * 2.0 ** -22)
     back = lambda v, *tail: torch.stack(v).view(n, T, H, *tail)  # noqa: E731
     return back(outs, LATENT), back(lses), back(eo, LATENT), back(el)
