@@ -49,12 +49,13 @@ struct Layout {
     static constexpr uint32_t PARTS = CODES ? 3 : 2;                            // in which its products are issued
     static constexpr uint32_t ROPE_PIECE = CODES ? BODY / 2 : BODY;             // of a tile: the rotated numbers (behind 128 or 64 numbers a line)
     static constexpr uint32_t TILE_BYTES = (ROPE_PIECE + 1) * PIECE;
-    // (queries: 8 pieces, of high and low halves in turn for codes, and the rotated one's.)  Weights take the place of the tile's rotated
-    // numbers, read by then.
-    static constexpr uint32_t AT_Q = 0, AT_TILES = (BODY + 1) * PIECE, AT_VALUES = AT_TILES + 2 * TILE_BYTES, AT_SCALES = AT_VALUES + (CODES ? BODY * PIECE : 0);
-    static constexpr uint32_t AT_UNITS = AT_SCALES + (CODES ? 2 * 4 * TILE * 4 : 0);                                  // of the tiles' rows
-    static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE * 4, AT_TOPS = AT_SEEN + 16, AT_ALPHA = AT_TOPS + 2 * ROW_WARPS * 4, AT_PEAK = AT_ALPHA + GROUP * 4;
-    static constexpr uint32_t AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 112;
+    // (queries: 8 pieces, of high and low halves in turn for codes, and the rotated one's.)  Weights have a place of their own beside codes,
+    // which are overwritten as soon as scores are there; else they take that of the tile's rotated numbers, read by then.
+    static constexpr uint32_t AT_Q = 0, AT_TILES = (BODY + 1) * PIECE, AT_VALUES = AT_TILES + 2 * TILE_BYTES, AT_WEIGHTS = AT_VALUES + (CODES ? BODY * PIECE : 0);
+    static constexpr uint32_t AT_SCALES = AT_WEIGHTS + (CODES ? PIECE : 0), AT_UNITS = AT_SCALES + (CODES ? 2 * 4 * TILE * 4 : 0);
+    static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE,              // (units of the tiles' rows: powers of two, by their exponents)
+ AT_TOPS = AT_SEEN + 16, AT_ALPHA = AT_TOPS + 2 * ROW_WARPS * 4, AT_PEAK = AT_ALPHA + GROUP * 4;
+    static constexpr uint32_t AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 80;
     static constexpr uint32_t AT_UNIT = AT_ALPHA;                               // the queries' units, until the softmax warps have read them
     // once all products are through: O in 32 bits [heads][512], the blocks' shares in it, the running maxima and the sums of two halves
     static constexpr uint32_t AT_OUT = AT_TILES, AT_SHARE = AT_OUT + GROUP * LATENT * 4, AT_MOST = AT_SHARE + MAX_CLUSTER * GROUP * 4, AT_SUM = AT_MOST + GROUP * 4;
@@ -63,8 +64,8 @@ struct Layout {
 constexpr uint32_t SHARED_MOST = Layout<AVSG_ROW_FP8>::TOTAL;
 
 // Barriers, by their place: half of a tile laid out (two of two tiles); tile read (2); step of S there, read (2 each); weights there (2); values
-// there; queries there.
-constexpr uint32_t FULL = 0, FREE = 32, SUM_FULL = 48, SUM_FREE = 64, WEIGHTS = 80, VALUES = 96, QUERIES = 104;
+// there; queries there; codes read by the matrix unit (2).
+constexpr uint32_t FULL = 0, FREE = 32, SUM_FULL = 48, SUM_FREE = 64, WEIGHTS = 80, VALUES = 96, QUERIES = 104, CODES_READ = 112;
 
 // TMEM columns: O^T in four parts of 128 numbers, then the sums S.
 constexpr uint32_t COL_OUT = 0, COL_S = 256, COLUMNS = 512;
@@ -81,7 +82,7 @@ struct Misc {
     int32_t last[WARPS];
     float unit;                         // what O's weights are multiples of
 };
-static_assert(sizeof(Misc) <= 112, "");
+static_assert(sizeof(Misc) <= 80, "");
 
 // Waits, bounded: false (and the block's other waits end too) if nothing came.  All lanes of a warp look together, in one instruction: 20
 // clocks where the phase is over.  (One lane looking for the others: 400, coming together again.)
@@ -153,14 +154,27 @@ __device__ __forceinline__ void convert(const RowPart& v, uint32_t sub, uint4 (&
     for (int i = 0; i < 4; ++i) {
         const uint32_t w[4] = {v.body[i].x, v.body[i].y, v.body[i].z, v.body[i].w};
         const uint32_t e = s[i] >> (8 * sub) & 255u;
-        const int field = (int)e - unit + 15;                                   // of scale / unit as fp16; below its range: zero
-        const uint32_t one = e == 255u ? 0x7E00u : field > 0 ? (uint32_t)field << 10 : field > -10 ? 1u << (field + 9) : 0u, ratio = one | one << 16;
+        const int power = (int)e - unit;                                        // scale / unit is 2^power, power <= 13
+        if (power >= -13 && e != 255u) {
+            // The upper bytes of 0, .5, 1, 1.5 and 2, 3, 4, 6 times 2^power as fp16 (the lower are zero), looked up by a code's last three bits, four
+            // codes at a time; signs beside.  (A conversion and a product for two codes: a fifth more instructions.)
+            const uint32_t small = 0x3E3C3800u + (uint32_t)(4 * power) * 0x01010100u, large = 0x46444240u + (uint32_t)(4 * power) * 0x01010101u;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            uint32_t x[4];
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t even = w[u] << 4;
+                const uint32_t a = __byte_perm(small, large, w[u] & 0x7777u) | (__byte_perm(even, w[u], 0xD9C8) & 0x80808080u);
+                const uint32_t b = __byte_perm(small, large, w[u] >> 16 & 0x7777u) | (__byte_perm(even, w[u], 0xFBEA) & 0x80808080u);
+                to[4 * i + u] = make_uint4(__byte_perm(a, 0, 0x1404), __byte_perm(a, 0, 0x3424), __byte_perm(b, 0, 0x1404), __byte_perm(b, 0, 0x3424));
+            }
+        } else {                                                                // below fp16's full digits, or no number
+            const uint32_t one = e == 255u ? 0x7E00u : power > -25 ? 1u << (power + 24) : 0u, ratio = one | one << 16;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = bits(__hmul2(e2m1_pair(w[u] >> (8 * j) & 255u), *reinterpret_cast<const __half2*>(&ratio)));
-            to[4 * i + u] = make_uint4(x[0], x[1], x[2], x[3]);
+            for (int u = 0; u < 4; ++u) {
+                uint32_t x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = bits(__hmul2(e2m1_pair(w[u] >> (8 * j) & 255u), *reinterpret_cast<const __half2*>(&ratio)));
+                to[4 * i + u] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
         }
     }
 }
@@ -228,6 +242,20 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             }
         }
     }
+    // A row warp's first two slots too (see there).
+    const uint32_t line_of_rows = ((warp - SOFTMAX_WARPS) & 7u) * 8u + lane % 8u;
+    struct Place { int32_t slot, id; };
+    auto place_at = [&](uint32_t j) -> Place {
+        Place to = {-1, 0};
+        const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + line_of_rows;
+        if (k < p.topk) {
+            to.slot = __ldg(slots + k);
+            if (p.spans) to.id = __ldg(ids + k);
+        }
+        return to;
+    };
+    Place here = {-1, 0}, next = {-1, 0};
+    if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS) { here = place_at(0); next = place_at(1); }
     // The selection's last position: what is behind it (padding) costs nothing.
     int32_t last = -1;
     for (uint32_t k = threadIdx.x; k < p.topk; k += THREADS) if (slots[k] >= 0) last = (int32_t)k;
@@ -243,6 +271,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             barrier_init(bars + WEIGHTS + 8 * i, SOFTMAX_WARPS);
         }
         barrier_init(bars + VALUES, ROW_WARPS);
+        for (uint32_t i = 0; i < 2; ++i) barrier_init(bars + CODES_READ + 8 * i, 1);
         barrier_init(bars + QUERIES, WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -341,7 +370,10 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
         auto outgrown = [](float peak, float most) { return peak > most + LAZY || (most == -INFINITY && peak > -INFINITY); };
         auto meet = [] { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); };
         auto pair_at = [&](uint32_t at, uint32_t c) { return *reinterpret_cast<const float2*>(shared + at + 4u * (row + 8u * c)); };
-        auto unit_of = [&](uint32_t j, uint32_t c) { return pair_at(L::AT_UNITS + 4u * TILE * (j & 1u), c); };
+        auto unit_of = [&](uint32_t j, uint32_t c) {
+            const uint32_t two = *reinterpret_cast<const uint16_t*>(shared + L::AT_UNITS + TILE * (j & 1u) + row + 8u * c);
+            return make_float2(__uint_as_float((two & 255u) << 23), __uint_as_float(two >> 8 << 23));
+        };
         auto scale_of = [&](uint32_t j, uint32_t g, uint32_t c) { return pair_at(L::AT_SCALES + 4u * TILE * (4u * (j & 1u) + g), c); };
         float x[2][8];                                      // a tile's scores (log2), complete after its last step
         // Step g of tile j: a sum or two from TMEM.
@@ -434,8 +466,8 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     float now = 0.f;
 #pragma unroll
                     for (uint32_t w = 0; w < ROW_WARPS; ++w) now = fmaxf(now, reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * ROW_WARPS + w]);
-                    if (now > unit) {
-                        const float to = __uint_as_float((__float_as_uint(now) + 0x007FFFFFu) & 0xFF800000u);         // a power of two
+                    if (now > unit) {                       // (powers of two, both)
+                        const float to = now * 8.f;                             // (with room, so that the next larger row moves nothing)
                         less = unit / to;
                         unit = to;
                     }
@@ -492,9 +524,16 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     }
                 }
             }
+            // The next tile's first sums, if they are there: their place in TMEM is wanted.
+            bool early = false;
+            if (L::CODES && busy && j + 1 < tiles) {
+                const uint32_t step = (j + 1) * L::STEPS;
+                early = __all_sync(0xffffffffu, barrier_done(bars + SUM_FULL + 8 * (step % SLOTS), step / SLOTS & 1u));
+                if (early) take(j + 1, 0);
+            }
             if (busy) {
                 const float inverse = 1.f / unit;
-                const uint32_t piece = base + L::AT_TILES + b * L::TILE_BYTES + L::ROPE_PIECE * PIECE;
+                const uint32_t piece = base + (L::CODES ? L::AT_WEIGHTS : L::AT_TILES + b * L::TILE_BYTES + L::ROPE_PIECE * PIECE);
                 if (L::HALF)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -503,6 +542,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
 #pragma unroll
                         for (int k = 0; k < 2; ++k) if (k == 0 || two) pair[k][c] = bits(__hmul2(*reinterpret_cast<const __half2*>(&pair[k][c]), ratio));
                     }
+                if (L::CODES && j > 0) wait(bars + FREE + 8 * (b ^ 1u), (j - 1) >> 1 & 1u, misc);              // (the last ones are read)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     if (real[k])
@@ -512,8 +552,9 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             fence_for_matrix_unit();
             tmem_before_sync();
             arrive(bars + WEIGHTS + 8 * b, lane);
+            if (!early) take(j + 1, 0);
 #pragma unroll
-            for (uint32_t g = 0; g < L::STEPS; ++g) take(j + 1, g);
+            for (uint32_t g = 1; g < L::STEPS; ++g) take(j + 1, g);
         }
         if (tiles) wait(bars + FREE + 8 * ((tiles - 1) & 1u), (tiles - 1) >> 1 & 1u, misc);       // (the tiles' place is free then)
         meet();
@@ -531,21 +572,12 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
         if (threadIdx.x == 0) misc->unit = L::HALF ? unit : 1.f;
     } else if (warp < SOFTMAX_WARPS + ROW_WARPS) {
         // ---- rows: a lane has every fourth 16-byte unit of one of its warp's eight ----
-        const uint32_t line = (warp - SOFTMAX_WARPS) * 8u + lane % 8u, sub = lane / 8u;
+        const uint32_t line = line_of_rows, sub = lane / 8u;
         const uint8_t* rows = p.buffer + (uint64_t)(p.mapped ? p.table_id[table] : table) * p.table_stride;
         int32_t begin = INT32_MIN, end = INT32_MAX;
         if (p.spans) { begin = p.spans[2 * item]; end = p.spans[2 * item + 1]; }
         // The slot (and id) of a tile's line, asked for two tiles ahead; where its row is, once it is there.
-        struct Place { int32_t slot, id; };
-        auto place = [&](uint32_t j) -> Place {
-            Place to = {-1, 0};
-            const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + line;
-            if (j < tiles && k < p.topk) {
-                to.slot = __ldg(slots + k);
-                if (p.spans) to.id = __ldg(ids + k);
-            }
-            return to;
-        };
+        auto place = [&](uint32_t j) { return j < tiles ? place_at(j) : Place{-1, 0}; };
         auto row_of = [&](Place to) -> const uint8_t* {
             if (to.slot < 0 || (p.spans && (to.id < begin || to.id >= end))) return nullptr;
             if ((uint32_t)to.slot >= p.rows) { if (p.status) atomicOr(p.status, ST_BAD_SLOT); return nullptr; }
@@ -559,13 +591,12 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             fence_for_matrix_unit();
             arrive(bars + FULL + 16 * b + 8 * half, lane);
         };
-        Place here = place(0), next = place(1);
         auto put_top = [&](uint32_t b, float top) {
             top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));                // (not negative; a NaN, too)
             if (lane == 0) reinterpret_cast<float*>(shared + L::AT_TOPS)[b * ROW_WARPS + warp - SOFTMAX_WARPS] = top;
         };
         auto free = [&](uint32_t j) { return __all_sync(0xffffffffu, wait(bars + FREE + 8 * (j & 1u), j >> 1 & 1u, misc)); };       // tile j is read
-        float* units = reinterpret_cast<float*>(shared + L::AT_UNITS) + line;
+        uint8_t* units = shared + L::AT_UNITS + line;
         if constexpr (FORMAT == AVSG_ROW_FP4) {
             RowPart part;
             const uint8_t* row = row_of(here);
@@ -580,7 +611,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 if (j >= 2 && !free(j - 2)) break;
                 put_seen(b, row);
                 put_top(b, unit);
-                if (sub == 0) units[b * TILE] = unit;
+                if (sub == 0) units[b * TILE] = (uint8_t)(__float_as_uint(unit) >> 23);
                 put_half(body, 0, tile, line, sub);
                 announce(b, 0);
                 put_half(body, 1, tile, line, sub);
@@ -593,10 +624,11 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 get_row(part, row, sub);
             }
         } else if constexpr (L::CODES) {
-            // Codes are copied as they are; each lane makes values of those that it copied, which nobody else has to wait for.
-            float s[4], s_next[4];
-            auto copy = [&](uint32_t j) {                   // tile j, whose rows `here` has; its scales come to s_next
-                const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
+            // Codes are copied as they are, a tile ahead; each lane makes values of those that it copied, which nobody else has to wait for.
+            float s_next[4];
+            uint32_t seen_next = 0;
+            auto copy = [&](uint32_t j) {                   // tile j, whose rows `here` has
+                const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
                 const uint8_t* row = row_of(here);
                 const uint8_t* from = row ? row : p.buffer;                      // (a masked row's bytes are zeros, nothing is read)
                 const float4 v = row ? __ldg(reinterpret_cast<const float4*>(row + LATENT)) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -606,39 +638,48 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
 #pragma unroll
                 for (uint32_t u = 0; u < 2; ++u) copy16(place_of(tile + L::ROPE_PIECE * PIECE, line, 4 * u + sub), from + row_bytes_of(FORMAT) - 2 * ROPE + 16 * (4 * u + sub), !row);
                 copies_close();
-                put_seen(b, row);
+                seen_next = __ballot_sync(0xffffffffu, row != nullptr);          // (lanes 0-7: the eight rows)
                 here = next;
                 next = place(j + 2);
             };
             if (tiles) copy(0);
             for (uint32_t j = 0; j < tiles; ++j) {
                 const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = s_next[i];
-                const uint32_t unit = code_unit(s);
-                const bool seen = s[0] != 0.f || s[1] != 0.f || s[2] != 0.f || s[3] != 0.f;
-                reinterpret_cast<float*>(shared + L::AT_SCALES)[(4 * b + sub) * TILE + line] = sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
-                if (sub == 0) units[b * TILE] = seen ? __uint_as_float(unit) : 0.f;
-                put_top(b, seen ? __uint_as_float(unit) : 0.f);
                 copies_wait<0>();
+                uint32_t w[8][4];
+#pragma unroll
+                for (uint32_t u = 0; u < 8; ++u)
+                    asm volatile("ld.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3])
+                                 : "r"(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub)));
+                const float s[4] = {s_next[0], s_next[1], s_next[2], s_next[3]};
+                const uint32_t unit = s[0] != 0.f || s[1] != 0.f || s[2] != 0.f || s[3] != 0.f ? code_unit(s) : 0u;
+                reinterpret_cast<float*>(shared + L::AT_SCALES)[(4 * b + sub) * TILE + line] = sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
+                if (sub == 0) units[b * TILE] = (uint8_t)(unit >> 23);
+                put_top(b, __uint_as_float(unit));
+                if (lane == 0) shared[L::AT_SEEN + 8 * b + warp - SOFTMAX_WARPS] = (uint8_t)seen_next;
                 announce(b, 0);
-                if (j >= 1 && !free(j - 1)) break;
-                if (j + 1 < tiles) copy(j + 1);
-                // ratio of scale and unit as fp16; NaN where one is no number
+                if (j + 1 < tiles) {                        // into the other place, as soon as the scores of the tile there are through
+                    if (j >= 1 && !__all_sync(0xffffffffu, wait(bars + CODES_READ + 8 * (b ^ 1u), (j - 1) >> 1 & 1u, misc))) break;
+                    copy(j + 1);
+                }
+                // (converted while the last tile's values are still read)
                 const float inverse = __uint_as_float((254u << 23) - (unit & 0x7F800000u));
+                uint4 body[16];
 #pragma unroll
                 for (uint32_t u = 0; u < 8; ++u) {
+                    // ratio of scale and unit as fp16; NaN where one is no number
                     const __half2 ratio = __half2half2(__float2half_rn(unit < 0x7F800000u ? s[u / 2] * inverse : __uint_as_float(0x7FC00000u)));
-                    uint32_t w[4], x[8];
-                    asm volatile("ld.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                 : "r"(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub)));
+                    uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        x[i] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i / 2] >> (i % 2 * 16)), __NV_E4M3)), ratio));
-                    // numbers 64 u + 16 sub ..
-                    put16(place_of(base + L::AT_VALUES + u * PIECE, line, 2 * sub), make_uint4(x[0], x[1], x[2], x[3]));
-                    put16(place_of(base + L::AT_VALUES + u * PIECE, line, 2 * sub + 1), make_uint4(x[4], x[5], x[6], x[7]));
+                        x[i] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[u][i / 2] >> (i % 2 * 16)), __NV_E4M3)), ratio));
+                    body[2 * u] = make_uint4(x[0], x[1], x[2], x[3]);
+                    body[2 * u + 1] = make_uint4(x[4], x[5], x[6], x[7]);
                 }
+                if (j >= 1 && !free(j - 1)) break;
+                // numbers 64 u + 16 sub ..
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) put16(place_of(base + L::AT_VALUES + i / 2 * PIECE, line, 2 * sub + i % 2), body[i]);
                 fence_for_matrix_unit();
                 arrive(bars + VALUES, lane);
             }
@@ -698,10 +739,11 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                                             ROPE_SHAPE, FORMAT == AVSG_ROW_BF16 || i > 0);
             }
             if (L::CODES || part == L::PARTS - 1) products_done(bars + SUM_FULL + 8 * (step % SLOTS));
+            if (L::CODES && part == L::PARTS - 1) products_done(bars + CODES_READ + 8 * (j & 1u));
         };
         auto add = [&](uint32_t j) {
             const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
-            const uint32_t rows = operand(L::CODES ? base + L::AT_VALUES : tile, PIECE), weights = operand(tile + L::ROPE_PIECE * PIECE, 16);
+            const uint32_t rows = operand(L::CODES ? base + L::AT_VALUES : tile, PIECE), weights = operand(L::CODES ? base + L::AT_WEIGHTS : tile + L::ROPE_PIECE * PIECE, 16);
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) {
                 const uint32_t part = i / 4, k = i % 4;
@@ -790,30 +832,37 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
     }
     __syncthreads();
     uint8_t* out = p.out + table * p.out_stride[0] + token * p.out_stride[1] + first_head * p.out_stride[2];
-    if (!misc->failed)
-        for (uint32_t u = rank * THREADS + threadIdx.x; u < heads * (LATENT / 8); u += p.cluster * THREADS) {
-            const uint32_t h = u / (LATENT / 8), d = u % (LATENT / 8);
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            float4 v[MAX_CLUSTER][2];
+    if (!misc->failed) {
+        if (p.cluster == 1) {
+            const float* from = reinterpret_cast<const float*>(shared + L::AT_OUT);
+#pragma unroll 4
+            for (uint32_t u = threadIdx.x; u < heads * (LATENT / 4); u += THREADS) {
+                const uint32_t h = u / (LATENT / 4), d = u % (LATENT / 4);
+                const float w = share[h];
+                const float4 v = w == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : reinterpret_cast<const float4*>(from)[u];      // (without rows there are no sums)
+                *reinterpret_cast<uint2*>(out + h * p.out_stride[2] + 8 * d) = make_uint2(bf16_pair(w * v.x, w * v.y), bf16_pair(w * v.z, w * v.w));
+            }
+        } else {
+            for (uint32_t u = rank * THREADS + threadIdx.x; u < heads * (LATENT / 4); u += p.cluster * THREADS) {
+                const uint32_t h = u / (LATENT / 4), d = u % (LATENT / 4);
+                float4 v[MAX_CLUSTER];
 #pragma unroll
-            for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
-                if (c < p.cluster) {
-                    const uint32_t at = in_block(base + L::AT_OUT + (h * LATENT + 8 * d) * 4u, c);
-                    v[c][0] = load_float4(at);
-                    v[c][1] = load_float4(at + 16);
-                }
+                for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
+                    if (c < p.cluster) v[c] = load_float4(in_block(base + L::AT_OUT + 16 * u, c));
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
-                if (c < p.cluster) {
-                    const float w = share[c * GROUP + h];
-                    if (w == 0.f) continue;                     // (a block without rows has no sums either)
-                    x[0] += w * v[c][0].x; x[1] += w * v[c][0].y; x[2] += w * v[c][0].z; x[3] += w * v[c][0].w;
-                    x[4] += w * v[c][1].x; x[5] += w * v[c][1].y; x[6] += w * v[c][1].z; x[7] += w * v[c][1].w;
-                }
-            *reinterpret_cast<uint4*>(out + h * p.out_stride[2] + 16 * d) =
-                make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+                for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
+                    if (c < p.cluster) {
+                        const float w = share[c * GROUP + h];
+                        if (w == 0.f) continue;
+                        x[0] += w * v[c].x; x[1] += w * v[c].y; x[2] += w * v[c].z; x[3] += w * v[c].w;
+                    }
+                *reinterpret_cast<uint2*>(out + h * p.out_stride[2] + 8 * d) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+            }
         }
-    else if (threadIdx.x == 0 && p.status) atomicOr(p.status, ST_WAIT_TIMEOUT);
+    } else if (threadIdx.x == 0 && p.status) {
+        atomicOr(p.status, ST_WAIT_TIMEOUT);
+    }
     __syncthreads();
     if (p.cluster > 1) cluster_sync();                          // nobody leaves whose memory is still read
 }
@@ -829,7 +878,7 @@ Kernel attend_kernel(uint32_t format, bool shaped)
     return k[format][shaped];
 }
 
-// Clusters of 2, 4, 8 blocks that a device runs at once (blocks of a cluster share a GPC), as found by attend_prepare().
+// Clusters of 1, 2, 4, 8 blocks that a device runs at once (blocks of a cluster share a GPC), as found by attend_prepare().
 constexpr int MAX_DEVICES = 64;
 std::atomic<int> g_active[MAX_DEVICES][4];
 
@@ -854,7 +903,7 @@ cudaError_t attend_prepare()
         for (int s = 0; s < 2; ++s)
             if ((e = cudaFuncSetAttribute(attend_kernel(f, s), cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_MOST)) != cudaSuccess) return e;
     if (device < 0 || device >= MAX_DEVICES) return cudaSuccess;                        // (then a block per query)
-    for (int i = 1; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {
         cudaLaunchAttribute attr;
         const cudaLaunchConfig_t c = config(1u << i, 1u << i, &attr, nullptr);
         int n = 0;
@@ -866,17 +915,22 @@ cudaError_t attend_prepare()
 
 cudaError_t launch_attend(AttendParams& p, uint32_t format, cudaStream_t stream)
 {
-    p.groups = (p.heads + GROUP - 1) / GROUP;
-    p.group_heads = (p.heads + p.groups - 1) / p.groups;
-    const uint64_t work = (uint64_t)p.n * p.n_tokens * p.groups;
-    // As many blocks per query as find room at once, each with a tile or more.
+    // Blocks of a query: its rows over a cluster's, its heads in groups; as many as find room at once.  First the rows, a tile or more to
+    // a block; then smaller groups of heads, down to 16, although each gathers the rows again: a block's sums travel between a cluster's blocks, heads x 2 KB.
+    const uint32_t least = (p.heads + GROUP - 1) / GROUP, tiles = (p.topk + TILE - 1) / TILE;
+    const uint64_t queries = (uint64_t)p.n * p.n_tokens;
     int device = -1;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
-    p.cluster = 1;
+    uint32_t log = 0;
     if (device >= 0 && device < MAX_DEVICES)
-        for (uint32_t i = 3; i > 0; --i)
-            if (work <= (uint64_t)g_active[device][i] && p.topk > TILE * ((1u << i) - 1u)) { p.cluster = 1u << i; break; }
+        for (log = 3; log > 0; --log) if (queries * least <= (uint64_t)g_active[device][log] && tiles >= 1u << log) break;
+    p.cluster = 1u << log;
+    p.groups = least;
+    while (device >= 0 && device < MAX_DEVICES && p.heads > 16u * p.groups && queries * p.groups * 2 <= (uint64_t)g_active[device][log]) p.groups *= 2;
+    p.group_heads = (p.heads + p.groups - 1) / p.groups;
+    p.groups = (p.heads + p.group_heads - 1) / p.group_heads;
+    const uint64_t work = queries * p.groups;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t c = config((uint32_t)(work * p.cluster), p.cluster, &attr, stream);
     void* args[] = {&p};
