@@ -570,12 +570,21 @@ def step_noalloc(tok, life, buffer, indices, kv, verified_len, *, max_lifetime: 
         _check(rc, "avsg_step_noalloc")
 
 
+_ROW_BYTES = {}
+
+
 def row_bytes(row_format: int) -> int:
     """Bytes of a row of that format: 1152, 656, 400."""
-    n = load_library().avsg_row_bytes(row_format)
-    if not n:
-        raise AvsgError(EINVAL, "row_bytes: no such row format: %r" % (row_format,))
+    n = _ROW_BYTES.get(row_format)
+    if n is None:
+        n = load_library().avsg_row_bytes(row_format)
+        if not n:
+            raise AvsgError(EINVAL, "row_bytes: no such row format: %r" % (row_format,))
+        _ROW_BYTES[row_format] = n
     return n
+
+
+_ROPE = struct.Struct("=32dfI")
 
 
 class Rope:
@@ -583,10 +592,11 @@ class Rope:
     neighbours, or (halves) 32 apart."""
 
     def __init__(self, inv_freq: Sequence[float], scale: float = 1.0, halves: bool = False):
-        inv_freq = [float(f) for f in inv_freq]
-        if len(inv_freq) != ROPE_DIMS // 2:
-            raise AvsgError(EINVAL, "Rope: inv_freq holds %d numbers, not %d" % (len(inv_freq), ROPE_DIMS // 2))
-        self.c = AvsgRope((ctypes.c_double * 32)(*inv_freq), float(scale), int(bool(halves)))
+        try:
+            self.c = AvsgRope.from_buffer_copy(_ROPE.pack(*inv_freq, scale, 1 if halves else 0))
+        except struct.error:
+            raise AvsgError(EINVAL, "Rope: inv_freq holds %d numbers, scale is one" % (ROPE_DIMS // 2)) from None
+        self.address = ctypes.addressof(self.c)
 
 
 def _need(ok, what: str) -> None:
@@ -594,20 +604,45 @@ def _need(ok, what: str) -> None:
         raise AvsgError(EINVAL, what)
 
 
-def _device_tensor(x, name: str, dtype, shape, device):
-    """Address of a contiguous device tensor of that type and shape."""
-    _need(x.dtype == dtype and tuple(x.shape) == tuple(shape) and x.device == device and x.is_contiguous(),
-          "%s: expected a contiguous %s tensor %s on %s, got %s %s on %s" % (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
-    return x.data_ptr()
+def _tensor_at(x, name: str, dtype, shape, device: int) -> int:
+    """Address of a contiguous tensor of that type and shape on that device."""
+    if x.dtype is dtype and x.shape == shape and x.get_device() == device and x.is_contiguous():
+        return x.data_ptr()
+    raise AvsgError(EINVAL, "%s: expected a contiguous %s tensor %s on cuda:%d, got %s %s on %s" %
+                    (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
 
 
-def _stream_of(stream, device):
+def _steps(x, size: int, dims: int):
+    """Bytes between the elements of each of the first dimensions (one of a single element may have any stride)."""
+    return [size * d if n > 1 else 0 for n, d in zip(x.shape[:dims], x.stride())]
+
+
+_raw_stream = None
+
+
+def _stream_of(stream, device: int) -> int:
     """Handle of the stream of a call whose tensors lie on `device`: by default that device's current one."""
+    global _raw_stream
     if stream is not None:
-        return _stream_handle(stream)
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return (raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream) or None
+        return _stream_handle(stream) or 0
+    if _raw_stream is None:
+        import torch
+        torch.cuda.init()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(device)
+
+
+# The argument blocks, packed at once: a structure of ctypes filled field by field costs a microsecond for eight of them.
+_APPEND = struct.Struct("=4I3Q2Q2Q4QQ5Q")
+_ATTEND = struct.Struct("=6I5Q3QQ3QQ2f6Q")
+_ROWS_CALL = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p)
+_append_fn = _attend_fn = None
+
+
+def _rows_functions():
+    global _append_fn, _attend_fn
+    lib = load_library()
+    _append_fn, _attend_fn = _ROWS_CALL(_address_of(lib.avsg_append)), _ROWS_CALL(_address_of(lib.avsg_attend))
 
 
 def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[Rope] = None, rows=None, row_stride=None, kv_rows=None,
@@ -620,53 +655,52 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     table, as avsg_step takes them; a tensor [rows, bytes] is a pool that all tables share.  Returns the values tensor (bf16 [n,
     n_tokens, 576], what the rows stand for) where one is wanted, else None."""
     import torch
-    a = AvsgAppendArgs()
-    device = latent.device
-    _need(latent.is_cuda and latent.dim() == 3 and latent.shape[2] == LATENT_DIMS, "append: latent is a CUDA tensor [n, n_tokens, 512]")
-    n, n_tokens = latent.shape[0], latent.shape[1]
-    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-    _need(latent.dtype in kinds and rope_part.dtype == latent.dtype and rope_part.device == device and
-          tuple(rope_part.shape) == (n, n_tokens, ROPE_DIMS) and latent.stride(2) == 1 and rope_part.stride(2) == 1,
-          "append: rope_part is a tensor [n, n_tokens, 64] of latent's type and device, both with their last numbers side by side")
-    size = latent.element_size()
-    a.n, a.n_tokens, a.row_format, a.type = n, n_tokens, row_format, kinds[latent.dtype]
-    a.latent, a.rope_part = latent.data_ptr(), rope_part.data_ptr()
-    # (a dimension of one may have any stride)
-    for to, x in ((a.latent_stride, latent), (a.rope_stride, rope_part)):
-        to[0] = x.stride(0) * size if n > 1 else 0
-        to[1] = x.stride(1) * size if n_tokens > 1 else 0
-    a.positions = _device_tensor(positions, "append: positions", torch.int32, (n, n_tokens), device)
-    if rows is not None:
-        a.rows = _device_tensor(rows, "append: rows", torch.int32, (n, n_tokens), device)
+    if _append_fn is None:
+        _rows_functions()
+    device, dtype, shape = latent.get_device(), latent.dtype, latent.shape
+    if device < 0 or len(shape) != 3 or shape[2] != LATENT_DIMS or latent.stride(2) != 1:
+        raise AvsgError(EINVAL, "append: latent is a CUDA tensor [n, n_tokens, 512] with its last numbers side by side")
+    n, n_tokens, _ = shape
+    kind = 0 if dtype is torch.bfloat16 else 1 if dtype is torch.float16 else 2 if dtype is torch.float32 else -1
+    if kind < 0 or rope_part.dtype is not dtype or rope_part.get_device() != device or rope_part.shape != (n, n_tokens, ROPE_DIMS) or \
+            rope_part.stride(2) != 1:
+        raise AvsgError(EINVAL, "append: rope_part is a tensor [n, n_tokens, 64] of latent's type (bf16, fp16, fp32) and device, with its last "
+                                "numbers side by side")
+    size = 4 if kind == 2 else 2
+    here = (n, n_tokens)
+    kv_base = at = table_step = 0
     keep = []
     if hasattr(kv, "data_ptr") and not isinstance(kv, (list, tuple)):
-        _need(kv.dtype == torch.uint8 and kv.dim() in (2, 3) and kv.stride(-1) == 1 and kv.shape[-1] == row_bytes(row_format) and
-              (kv.dim() == 2 or kv.shape[0] == n) and (kv.device == device or not kv.is_cuda),
-              "append: kv is a uint8 tensor [n, rows, row bytes] or [rows, row bytes] on latent's device or pinned, or a list of caches")
+        full = kv.shape
+        bytes_ = row_bytes(row_format)
+        if kv.dtype is not torch.uint8 or len(full) not in (2, 3) or full[-1] != bytes_ or kv.stride(-1) != 1 or \
+                (len(full) == 3 and full[0] != n) or (kv.is_cuda and kv.get_device() != device):
+            raise AvsgError(EINVAL, "append: kv is a uint8 tensor [n, rows, row bytes] or [rows, row bytes] on latent's device or pinned, or a "
+                                    "list of caches")
         _need(row_stride is None, "append: row_stride goes with a list of caches")
-        a.kv, a.kv_table_stride = kv.data_ptr(), (kv.stride(0) if kv.dim() == 3 and n > 1 else 0)
+        at, table_step = kv.data_ptr(), (kv.stride(0) if len(full) == 3 and n > 1 else 0)
         if kv_rows is None:
-            kv_rows = [kv.shape[-2]] * n
-        if kv.shape[-2] > 1 and kv.stride(-2) != kv.shape[-1]:
+            kv_rows = [full[-2]] * n
+        if full[-2] > 1 and kv.stride(-2) != bytes_:
             row_stride = [kv.stride(-2)] * n
     else:
         kv = list(kv)
         _need(len(kv) == n, "append: one cache per table")
-        owner, a.kv_base = _c_array("Q", [_addr(k) for k in kv], n)
+        owner, kv_base = _c_array("Q", [_addr(k) for k in kv], n)
         keep.append(owner)
-    for name, kind, given in (("row_stride", "Q", row_stride), ("kv_rows", "I", kv_rows), ("table_ids", "I", _tables)):
-        owner, at = _c_array(kind, given, n)
-        keep.append(owner)
-        setattr(a, name, at)
-    if rope is not None:
-        a.rope = ctypes.addressof(rope.c)
+    strides, strides_at = _c_array("Q", row_stride, n)
+    limits, limits_at = _c_array("I", kv_rows, n)
+    tables, tables_at = _c_array("I", _tables, n)
     if want_values and values is None:
-        values = torch.empty((n, n_tokens, LATENT_DIMS + ROPE_DIMS), dtype=torch.bfloat16, device=device)
-    if values is not None:
-        a.values = _device_tensor(values, "append: values", torch.bfloat16, (n, n_tokens, LATENT_DIMS + ROPE_DIMS), device)
-    if status is not None:
-        a.status = _addr(status)
-    rc = load_library().avsg_append(_ctx._h if _ctx is not None else None, ctypes.byref(a), _stream_of(stream, device))
+        values = torch.empty((n, n_tokens, LATENT_DIMS + ROPE_DIMS), dtype=torch.bfloat16, device=latent.device)
+    block = _APPEND.pack(
+        n, n_tokens, row_format, kind, tables_at or 0, latent.data_ptr(), rope_part.data_ptr(), *_steps(latent, size, 2), *_steps(rope_part, size, 2),
+        _tensor_at(positions, "append: positions", torch.int32, here, device),
+        0 if rows is None else _tensor_at(rows, "append: rows", torch.int32, here, device), kv_base, at, table_step, strides_at or 0, limits_at or 0,
+        0 if rope is None else rope.address,
+        0 if values is None else _tensor_at(values, "append: values", torch.bfloat16, (n, n_tokens, LATENT_DIMS + ROPE_DIMS), device),
+        0 if status is None else _addr(status))
+    rc = _append_fn(None if _ctx is None else _ctx._h, block, _stream_of(stream, device))
     if rc != OK:
         _check(rc, "avsg_append")
     return values
@@ -682,50 +716,44 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     int32 [n, n_tokens] (a bias of slope * (id - position)); rope with positions: q's last 64 numbers are rotated here.
     Returns bf16 [n, n_tokens, heads, 512], and with want_lse the fp32 logarithms [n, n_tokens, heads] too."""
     import torch
-    a = AvsgAttendArgs()
-    device = q.device
-    _need(q.is_cuda and q.dtype == torch.bfloat16 and q.dim() == 4 and q.shape[3] == LATENT_DIMS + ROPE_DIMS and q.stride(3) == 1,
-          "attend: q is a bf16 CUDA tensor [n, n_tokens, heads, 576] with its last numbers side by side")
-    n, n_tokens, heads, _ = q.shape
+    if _attend_fn is None:
+        _rows_functions()
+    device, shape, bf16, int32 = q.get_device(), q.shape, torch.bfloat16, torch.int32
+    if device < 0 or q.dtype is not bf16 or len(shape) != 4 or shape[3] != LATENT_DIMS + ROPE_DIMS or q.stride(3) != 1:
+        raise AvsgError(EINVAL, "attend: q is a bf16 CUDA tensor [n, n_tokens, heads, 576] with its last numbers side by side")
+    n, n_tokens, heads, _ = shape
     _need(slots.dim() == 3, "attend: slots is [n, n_tokens, topk]")
     topk = slots.shape[2]
-    a.n, a.n_tokens, a.topk, a.heads, a.row_format = n, n_tokens, topk, heads, row_format
-    a.slots = _device_tensor(slots, "attend: slots", torch.int32, (n, n_tokens, topk), device)
+    ids_like, here = (n, n_tokens, topk), (n, n_tokens)
+    tables_at = rows_at = rows = row_step = 0
     if _ctx is None:
-        _need(buffer.is_cuda and buffer.device == device and buffer.dtype == torch.uint8 and buffer.dim() == 3 and buffer.shape[0] == n and
-              buffer.stride(2) == 1 and buffer.shape[2] == row_bytes(row_format) and
-              (n == 1 or buffer.stride(0) == buffer.stride(1) * buffer.shape[1]),
-              "attend: buffer is a uint8 tensor [n, slots, row bytes] on q's device, its tables one behind another")
-        a.buffer, a.buffer_slots, a.buffer_row_bytes = buffer.data_ptr(), buffer.shape[1], (buffer.stride(1) if buffer.shape[1] > 1 else 0)
+        held = buffer.shape
+        if buffer.get_device() != device or buffer.dtype is not torch.uint8 or len(held) != 3 or held[0] != n or held[2] != row_bytes(row_format) or \
+                buffer.stride(2) != 1 or (n > 1 and buffer.stride(0) != buffer.stride(1) * held[1]):
+            raise AvsgError(EINVAL, "attend: buffer is a uint8 tensor [n, slots, row bytes] on q's device, its tables one behind another")
+        rows_at, rows, row_step = buffer.data_ptr(), held[1], (buffer.stride(1) if held[1] > 1 else 0)
     else:
-        _need(len(_tables) == n, "attend: one table per query block")
-        owner, a.table_ids = _c_array("I", _tables, n)
+        _need(len(_tables) == n, "attend: one table per block of queries")
+        owner, tables_at = _c_array("I", _tables, n)
     if out is None:
-        out = torch.empty((n, n_tokens, heads, LATENT_DIMS), dtype=torch.bfloat16, device=device)
-    _need(out.dtype == torch.bfloat16 and out.device == device and tuple(out.shape) == (n, n_tokens, heads, LATENT_DIMS) and out.stride(3) == 1,
-          "attend: out is a bf16 tensor [n, n_tokens, heads, 512] on q's device with its last numbers side by side")
-    a.q, a.out = q.data_ptr(), out.data_ptr()
-    for to, x in ((a.q_stride, q), (a.out_stride, out)):
-        for i in range(3):
-            to[i] = 2 * x.stride(i) if x.shape[i] > 1 else 0
+        out = torch.empty((n, n_tokens, heads, LATENT_DIMS), dtype=bf16, device=q.device)
+        out_steps = (1024 * heads * n_tokens, 1024 * heads, 1024)
+    else:
+        if out.dtype is not bf16 or out.get_device() != device or out.shape != (n, n_tokens, heads, LATENT_DIMS) or out.stride(3) != 1:
+            raise AvsgError(EINVAL, "attend: out is a bf16 tensor [n, n_tokens, heads, 512] on q's device with its last numbers side by side")
+        out_steps = _steps(out, 2, 3)
     if want_lse and lse is None:
-        lse = torch.empty((n, n_tokens, heads), dtype=torch.float32, device=device)
-    if lse is not None:
-        a.lse = _device_tensor(lse, "attend: lse", torch.float32, (n, n_tokens, heads), device)
-    a.scale, a.softcap = scale, softcap
-    if ids is not None:
-        a.ids = _device_tensor(ids, "attend: ids", torch.int32, (n, n_tokens, topk), device)
-    if positions is not None:
-        a.positions = _device_tensor(positions, "attend: positions", torch.int32, (n, n_tokens), device)
-    if spans is not None:
-        a.spans = _device_tensor(spans, "attend: spans", torch.int32, (n, n_tokens, 2), device)
-    if slopes is not None:
-        a.slopes = _device_tensor(slopes, "attend: slopes", torch.float32, (heads,), device)
-    if rope is not None:
-        a.rope = ctypes.addressof(rope.c)
-    if status is not None:
-        a.status = _addr(status)
-    rc = load_library().avsg_attend(_ctx._h if _ctx is not None else None, ctypes.byref(a), _stream_of(stream, device))
+        lse = torch.empty((n, n_tokens, heads), dtype=torch.float32, device=q.device)
+    block = _ATTEND.pack(
+        n, n_tokens, topk, heads, row_format, rows, row_step, tables_at, rows_at, _tensor_at(slots, "attend: slots", int32, ids_like, device),
+        q.data_ptr(), *_steps(q, 2, 3), out.data_ptr(), *out_steps,
+        0 if lse is None else _tensor_at(lse, "attend: lse", torch.float32, (n, n_tokens, heads), device), scale, softcap,
+        0 if ids is None else _tensor_at(ids, "attend: ids", int32, ids_like, device),
+        0 if positions is None else _tensor_at(positions, "attend: positions", int32, here, device),
+        0 if spans is None else _tensor_at(spans, "attend: spans", int32, (n, n_tokens, 2), device),
+        0 if slopes is None else _tensor_at(slopes, "attend: slopes", torch.float32, (heads,), device),
+        0 if rope is None else rope.address, 0 if status is None else _addr(status))
+    rc = _attend_fn(None if _ctx is None else _ctx._h, block, _stream_of(stream, device))
     if rc != OK:
         _check(rc, "avsg_attend")
-    return (out, lse) if lse is not None else out
+    return out if lse is None else (out, lse)
