@@ -14,8 +14,8 @@
 // units of a power of two of the head's (exact: bf16 has 8 bits, fp16 11), weights fp16 in units of the largest row's.  The rotated 64 numbers are
 // bf16 on both sides and have a sum of their own.
 //
-// Warps: 0-7 softmax (two for each 16 heads, 32 rows each), 8-15 rows (each gathers 8 of a tile's, a tile ahead, in registers or by asynchronous
-// copies, and converts them), 16 issues the products, whichever of the next tile's S and the last one's O can be next.
+// Warps: 0-7 softmax (two for each 16 heads, 32 rows each); 8-15 rows, gathered and converted by four warps for one tile and four for the next (bf16: by
+// all eight), so that one's loads are under way while the other stores; 16 issues the products, whichever of the next tile's S and the last one's O can be next.
 //
 // A query's rows are split over a cluster's blocks where queries are few, tile by tile in turn; the blocks' sums are joined through
 // distributed shared memory in a fixed order (same results on every run, no workspace).
@@ -45,6 +45,7 @@ template <uint32_t FORMAT>
 struct Layout {
     static constexpr bool HALF = FORMAT != AVSG_ROW_BF16;                       // fp16 weights and values
     static constexpr bool CODES = FORMAT == AVSG_ROW_FP8;                       // scores from e4m3 codes
+    static constexpr uint32_t TURNS = FORMAT == AVSG_ROW_FP4 ? 2 : 1;           // groups of row warps that take tiles in turn
     static constexpr uint32_t STEPS = CODES ? 3 : 1;                            // of a tile's S: two latent sums, two, the rotated one; or all at once
     static constexpr uint32_t PARTS = CODES ? 3 : 2;                            // in which its products are issued
     static constexpr uint32_t ROPE_PIECE = CODES ? BODY / 2 : BODY;             // of a tile: the rotated numbers (behind 128 or 64 numbers a line)
@@ -54,7 +55,7 @@ struct Layout {
     static constexpr uint32_t AT_Q = 0, AT_TILES = (BODY + 1) * PIECE, AT_VALUES = AT_TILES + 2 * TILE_BYTES, AT_WEIGHTS = AT_VALUES + (CODES ? BODY * PIECE : 0);
     static constexpr uint32_t AT_SCALES = AT_WEIGHTS + (CODES ? PIECE : 0), AT_UNITS = AT_SCALES + (CODES ? 2 * 4 * TILE * 4 : 0);
     static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE,              // (units of the tiles' rows: powers of two, by their exponents)
- AT_TOPS = AT_SEEN + 16, AT_ALPHA = AT_TOPS + 2 * ROW_WARPS * 4, AT_PEAK = AT_ALPHA + GROUP * 4;
+ AT_TOPS = AT_SEEN + 16, TOPS = ROW_WARPS / TURNS, AT_ALPHA = AT_TOPS + 2 * TOPS * 4, AT_PEAK = AT_ALPHA + GROUP * 4;
     static constexpr uint32_t AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 80;
     static constexpr uint32_t AT_UNIT = AT_ALPHA;                               // the queries' units, until the softmax warps have read them
     // once all products are through: O in 32 bits [heads][512], the blocks' shares in it, the running maxima and the sums of two halves
@@ -71,9 +72,10 @@ constexpr uint32_t FULL = 0, FREE = 32, SUM_FULL = 48, SUM_FREE = 64, WEIGHTS = 
 constexpr uint32_t COL_OUT = 0, COL_S = 256, COLUMNS = 512;
 
 constexpr float LOG2E = 1.4426950408889634f;
-// The maximum that weights refer to lags behind by up to LAZY (log2), so that O is rescaled seldom; and they are 2^ROOM times as large:
-// as fp16 the largest is 2^4 to 2^15, and all are whole to 2^-25.
-constexpr float LAZY = 11.f, ROOM = 4.f;
+// The maximum that weights refer to lags behind by up to LAZY (log2), so that O is rescaled seldom (bf16 has the range for much more).  fp16
+// weights are 2^ROOM times as large: the largest is 2^4 to 2^15, and all are whole to 2^-25.
+template <uint32_t FORMAT> constexpr float LAZY = Layout<FORMAT>::HALF ? 11.f : 60.f;
+constexpr float ROOM = 4.f;
 constexpr uint32_t LEAST_UNIT = 27u << 23;                  // 2^-100: no row's unit is smaller, so that ratios of units stay finite
 constexpr long long WAIT_CLOCKS = 1ll << 29;                // about 0.3 s: longer than any wait that ends
 
@@ -145,14 +147,15 @@ __device__ __forceinline__ uint32_t nibble_unit(uint4 scales)
     return (uint32_t)max((int)most - 13, (int)(LEAST_UNIT >> 23));
 }
 
-// A lane's part of such a row as fp16: what goes to unit 4 (sub % 2) + u of piece 2 i + sub / 2.
-__device__ __forceinline__ void convert(const RowPart& v, uint32_t sub, uint4 (&to)[16])
+// Lays half of a lane's part of such a row out as line `line` of a tile, as fp16: 32 numbers go to units 4 (sub % 2) .. of piece 2 i + sub / 2.  The eight
+// lanes of a store's phase have the eight lines of a piece: no two share a bank.
+__device__ __forceinline__ void put_half(const RowPart& v, int half, uint32_t tile, uint32_t line, uint32_t sub)
 {
     const uint32_t s[4] = {v.scales.x, v.scales.y, v.scales.z, v.scales.w};
     const int unit = (int)nibble_unit(v.scales);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w[4] = {v.body[i].x, v.body[i].y, v.body[i].z, v.body[i].w};
+    for (int i = 2 * half; i < 2 * half + 2; ++i) {
+        const uint32_t w[4] = {v.body[i].x, v.body[i].y, v.body[i].z, v.body[i].w}, piece = tile + (2 * i + sub / 2) * PIECE;
         const uint32_t e = s[i] >> (8 * sub) & 255u;
         const int power = (int)e - unit;                                        // scale / unit is 2^power, power <= 13
         if (power >= -13 && e != 255u) {
@@ -164,7 +167,8 @@ __device__ __forceinline__ void convert(const RowPart& v, uint32_t sub, uint4 (&
                 const uint32_t even = w[u] << 4;
                 const uint32_t a = __byte_perm(small, large, w[u] & 0x7777u) | (__byte_perm(even, w[u], 0xD9C8) & 0x80808080u);
                 const uint32_t b = __byte_perm(small, large, w[u] >> 16 & 0x7777u) | (__byte_perm(even, w[u], 0xFBEA) & 0x80808080u);
-                to[4 * i + u] = make_uint4(__byte_perm(a, 0, 0x1404), __byte_perm(a, 0, 0x3424), __byte_perm(b, 0, 0x1404), __byte_perm(b, 0, 0x3424));
+                put16(place_of(piece, line, 4 * (sub % 2) + u),
+                      make_uint4(__byte_perm(a, 0, 0x1404), __byte_perm(a, 0, 0x3424), __byte_perm(b, 0, 0x1404), __byte_perm(b, 0, 0x3424)));
             }
         } else {                                                                // below fp16's full digits, or no number
             const uint32_t one = e == 255u ? 0x7E00u : power > -25 ? 1u << (power + 24) : 0u, ratio = one | one << 16;
@@ -173,17 +177,10 @@ __device__ __forceinline__ void convert(const RowPart& v, uint32_t sub, uint4 (&
                 uint32_t x[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = bits(__hmul2(e2m1_pair(w[u] >> (8 * j) & 255u), *reinterpret_cast<const __half2*>(&ratio)));
-                to[4 * i + u] = make_uint4(x[0], x[1], x[2], x[3]);
+                put16(place_of(piece, line, 4 * (sub % 2) + u), make_uint4(x[0], x[1], x[2], x[3]));
             }
         }
     }
-}
-
-// Lays half of it out as line `line` of a tile.  The eight lanes of a store's phase have the eight lines of a piece: no two share a bank.
-__device__ __forceinline__ void put_half(const uint4 (&from)[16], int half, uint32_t tile, uint32_t line, uint32_t sub)
-{
-#pragma unroll
-    for (int i = 8 * half; i < 8 * half + 8; ++i) put16(place_of(tile + (i / 4 * 2 + sub / 2) * PIECE, line, 4 * (sub % 2) + i % 4), from[i]);
 }
 
 // The unit that an e4m3 row's values are in: the power of two at or above its largest scale, / 128, so that they reach 448 x 128 = 57344.
@@ -242,20 +239,27 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             }
         }
     }
-    // A row warp's first two slots too (see there).
-    const uint32_t line_of_rows = ((warp - SOFTMAX_WARPS) & 7u) * 8u + lane % 8u;
+    // A row warp's first slots too, for its first two tiles: of a line a lane, or of two where warps take turns.
+    const uint32_t first_tile = L::TURNS > 1 ? (warp - SOFTMAX_WARPS) / 4u & 1u : 0u;
+    const uint32_t line = L::TURNS > 1 ? (warp & 3u) * 16u + lane % 8u : (warp & 7u) * 8u + lane % 8u;
     struct Place { int32_t slot, id; };
-    auto place_at = [&](uint32_t j) -> Place {
+    auto place_at = [&](uint32_t j, uint32_t at) -> Place {
         Place to = {-1, 0};
-        const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + line_of_rows;
+        const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + at;
         if (k < p.topk) {
             to.slot = __ldg(slots + k);
             if (p.spans) to.id = __ldg(ids + k);
         }
         return to;
     };
-    Place here = {-1, 0}, next = {-1, 0};
-    if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS) { here = place_at(0); next = place_at(1); }
+    Place here[2] = {{-1, 0}, {-1, 0}}, next[2] = {{-1, 0}, {-1, 0}};
+    if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS) {
+#pragma unroll
+        for (uint32_t i = 0; i < L::TURNS; ++i) {
+            here[i] = place_at(first_tile, line + 8u * i);
+            next[i] = place_at(first_tile + L::TURNS, line + 8u * i);
+        }
+    }
     // The selection's last position: what is behind it (padding) costs nothing.
     int32_t last = -1;
     for (uint32_t k = threadIdx.x; k < p.topk; k += THREADS) if (slots[k] >= 0) last = (int32_t)k;
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
     if (lane == 0) misc->last[warp] = last;
     if (threadIdx.x == 0) {
         misc->failed = 0;
-        for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, ROW_WARPS);
+        for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, ROW_WARPS / L::TURNS);
         for (uint32_t i = 0; i < 2; ++i) {
             barrier_init(bars + FREE + 8 * i, 1);
             barrier_init(bars + SUM_FULL + 8 * i, 1);
@@ -367,7 +371,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
         const int32_t position = SHAPED && p.slopes ? p.positions[item] : 0;
         float most[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f}, unit = __uint_as_float(LEAST_UNIT);
         const uint32_t lanes = tmem + (quarter * 32u << 16), row = 32u * half + 2u * quad;        // (this thread's rows: 8 c + i, c = 0 .. 3, i = 0, 1, from there)
-        auto outgrown = [](float peak, float most) { return peak > most + LAZY || (most == -INFINITY && peak > -INFINITY); };
+        auto outgrown = [](float peak, float most) { return peak > most + LAZY<FORMAT> || (most == -INFINITY && peak > -INFINITY); };
         auto meet = [] { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); };
         auto pair_at = [&](uint32_t at, uint32_t c) { return *reinterpret_cast<const float2*>(shared + at + 4u * (row + 8u * c)); };
         auto unit_of = [&](uint32_t j, uint32_t c) {
@@ -412,6 +416,16 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     }
                 }
         };
+        int32_t id[8];                                      // of this thread's rows, where scores have a bias by distance
+        auto ask_ids = [&](uint32_t j) {
+            if (SHAPED && busy && p.slopes)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const uint64_t at = (uint64_t)(rank + j * p.cluster) * TILE + row + 8 * (c / 2) + c % 2;
+                    id[c] = at < p.topk ? __ldg(ids + at) : 0;
+                }
+        };
+        ask_ids(0);
 #pragma unroll
         for (uint32_t g = 0; g < L::STEPS; ++g) take(0, g);
         for (uint32_t j = 0; j < tiles; ++j) {              // (also after a wait that failed: the warps meet at a barrier)
@@ -422,8 +436,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 if constexpr (SHAPED) {
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        const uint64_t at = (uint64_t)(rank + j * p.cluster) * TILE + row + 8 * (c / 2) + c % 2;
-                        const float away = p.slopes && at < p.topk ? (float)(__ldg(ids + at) - position) : 0.f;
+                        const float away = p.slopes ? (float)(id[c] - position) : 0.f;
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             if (k == 1 && !two) continue;
@@ -446,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     for (int c = 0; c < 8; ++c) peak[k] = fmaxf(peak[k], x[k][c]);
                     behind |= real[k] && outgrown(peak[k], most[k]);
                 }
-                if (L::HALF) behind |= reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * ROW_WARPS + lane % ROW_WARPS] > unit;
+                if (L::HALF) behind |= reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * L::TOPS + lane % L::TOPS] > unit;
             }
             // Weights would grow beyond their range: the references move, and O is brought to the new ones before it is added to.
             int any;
@@ -465,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 if (L::HALF) {
                     float now = 0.f;
 #pragma unroll
-                    for (uint32_t w = 0; w < ROW_WARPS; ++w) now = fmaxf(now, reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * ROW_WARPS + w]);
+                    for (uint32_t w = 0; w < L::TOPS; ++w) now = fmaxf(now, reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * L::TOPS + w]);
                     if (now > unit) {                       // (powers of two, both)
                         const float to = now * 8.f;                             // (with room, so that the next larger row moves nothing)
                         less = unit / to;
@@ -552,6 +565,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             fence_for_matrix_unit();
             tmem_before_sync();
             arrive(bars + WEIGHTS + 8 * b, lane);
+            ask_ids(j + 1);
             if (!early) take(j + 1, 0);
 #pragma unroll
             for (uint32_t g = 1; g < L::STEPS; ++g) take(j + 1, g);
@@ -572,116 +586,139 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
         if (threadIdx.x == 0) misc->unit = L::HALF ? unit : 1.f;
     } else if (warp < SOFTMAX_WARPS + ROW_WARPS) {
         // ---- rows: a lane has every fourth 16-byte unit of one of its warp's eight ----
-        const uint32_t line = line_of_rows, sub = lane / 8u;
+        const uint32_t sub = lane / 8u;
         const uint8_t* rows = p.buffer + (uint64_t)(p.mapped ? p.table_id[table] : table) * p.table_stride;
         int32_t begin = INT32_MIN, end = INT32_MAX;
         if (p.spans) { begin = p.spans[2 * item]; end = p.spans[2 * item + 1]; }
         // The slot (and id) of a tile's line, asked for two tiles ahead; where its row is, once it is there.
-        auto place = [&](uint32_t j) { return j < tiles ? place_at(j) : Place{-1, 0}; };
+        auto place = [&](uint32_t j, uint32_t at) { return j < tiles ? place_at(j, at) : Place{-1, 0}; };
         auto row_of = [&](Place to) -> const uint8_t* {
             if (to.slot < 0 || (p.spans && (to.id < begin || to.id >= end))) return nullptr;
             if ((uint32_t)to.slot >= p.rows) { if (p.status) atomicOr(p.status, ST_BAD_SLOT); return nullptr; }
             return rows + (uint64_t)to.slot * p.row_stride;
         };
-        auto put_seen = [&](uint32_t b, const uint8_t* row) {
-            const uint32_t seen = __ballot_sync(0xffffffffu, row != nullptr);               // (lanes 0-7: the eight rows)
-            if (lane == 0) shared[L::AT_SEEN + 8 * b + warp - SOFTMAX_WARPS] = (uint8_t)seen;
+        // (lanes 0-7 speak for eight rows)
+        auto put_seen = [&](uint32_t b, uint32_t eight, const uint8_t* row) {
+            const uint32_t seen = __ballot_sync(0xffffffffu, row != nullptr);
+            if (lane == 0) shared[L::AT_SEEN + 8 * b + eight] = (uint8_t)seen;
         };
         auto announce = [&](uint32_t b, uint32_t half) {
             fence_for_matrix_unit();
             arrive(bars + FULL + 16 * b + 8 * half, lane);
         };
+        const uint32_t group_warp = (warp - SOFTMAX_WARPS) % L::TOPS;
         auto put_top = [&](uint32_t b, float top) {
             top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));                // (not negative; a NaN, too)
-            if (lane == 0) reinterpret_cast<float*>(shared + L::AT_TOPS)[b * ROW_WARPS + warp - SOFTMAX_WARPS] = top;
+            if (lane == 0) reinterpret_cast<float*>(shared + L::AT_TOPS)[b * L::TOPS + group_warp] = top;
         };
-        auto free = [&](uint32_t j) { return __all_sync(0xffffffffu, wait(bars + FREE + 8 * (j & 1u), j >> 1 & 1u, misc)); };       // tile j is read
+        auto passed = [&](uint32_t bar, uint32_t j) { return __all_sync(0xffffffffu, wait(bars + bar + 8 * (j & 1u), j >> 1 & 1u, misc)); };    // of tile j
         uint8_t* units = shared + L::AT_UNITS + line;
-        if constexpr (FORMAT == AVSG_ROW_FP4) {
-            RowPart part;
-            const uint8_t* row = row_of(here);
-            get_row(part, row, sub);
-            for (uint32_t j = 0; j < tiles; ++j) {
-                const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
-                // (converted while the tile's place is still read)
-                uint4 body[16];
-                convert(part, sub, body);
-                const uint4 rope[2] = {part.rope[0], part.rope[1]};
-                const float unit = row ? __uint_as_float(nibble_unit(part.scales) << 23) : 0.f;
-                if (j >= 2 && !free(j - 2)) break;
-                put_seen(b, row);
-                put_top(b, unit);
-                if (sub == 0) units[b * TILE] = (uint8_t)(__float_as_uint(unit) >> 23);
-                put_half(body, 0, tile, line, sub);
-                announce(b, 0);
-                put_half(body, 1, tile, line, sub);
+        auto advance = [&](uint32_t j) {                    // the slots of this warp's next tile, and those behind asked for
 #pragma unroll
-                for (int i = 0; i < 2; ++i) put16(place_of(tile + L::ROPE_PIECE * PIECE, line, 4 * i + sub), rope[i]);
-                announce(b, 1);
-                here = next;
-                next = place(j + 2);
-                row = row_of(here);
-                get_row(part, row, sub);
+            for (uint32_t i = 0; i < L::TURNS; ++i) { here[i] = next[i]; next[i] = place(j + 2 * L::TURNS, line + 8u * i); }
+        };
+        if constexpr (FORMAT == AVSG_ROW_FP4) {
+            RowPart part[2];
+            const uint8_t* row[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { row[i] = row_of(here[i]); get_row(part[i], row[i], sub); }
+            for (uint32_t j = first_tile; j < tiles; j += 2) {
+                const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
+                float unit[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) unit[i] = row[i] ? __uint_as_float(nibble_unit(part[i].scales) << 23) : 0.f;
+                if (j >= 2 && !passed(FREE, j - 2)) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    put_seen(b, 2u * group_warp + i, row[i]);
+                    if (sub == 0) units[b * TILE + 8 * i] = (uint8_t)(__float_as_uint(unit[i]) >> 23);
+                }
+                put_top(b, fmaxf(unit[0], unit[1]));
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        put_half(part[i], half, tile, line + 8u * i, sub);
+                        if (half == 1)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) put16(place_of(tile + L::ROPE_PIECE * PIECE, line + 8u * i, 4 * u + sub), part[i].rope[u]);
+                    }
+                    announce(b, half);
+                }
+                advance(j);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { row[i] = row_of(here[i]); get_row(part[i], row[i], sub); }
             }
         } else if constexpr (L::CODES) {
             // Codes are copied as they are, a tile ahead; each lane makes values of those that it copied, which nobody else has to wait for.
-            float s_next[4];
-            uint32_t seen_next = 0;
+            float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);
+            const uint8_t* row = nullptr;
             auto copy = [&](uint32_t j) {                   // tile j, whose rows `here` has
                 const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
-                const uint8_t* row = row_of(here);
+                row = row_of(here[0]);
                 const uint8_t* from = row ? row : p.buffer;                      // (a masked row's bytes are zeros, nothing is read)
-                const float4 v = row ? __ldg(reinterpret_cast<const float4*>(row + LATENT)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                s_next[0] = v.x; s_next[1] = v.y; s_next[2] = v.z; s_next[3] = v.w;
+                scales = row ? __ldg(reinterpret_cast<const float4*>(row + LATENT)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (uint32_t u = 0; u < 8; ++u) copy16(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub), from + 16 * (4 * u + sub), !row);
 #pragma unroll
                 for (uint32_t u = 0; u < 2; ++u) copy16(place_of(tile + L::ROPE_PIECE * PIECE, line, 4 * u + sub), from + row_bytes_of(FORMAT) - 2 * ROPE + 16 * (4 * u + sub), !row);
                 copies_close();
-                seen_next = __ballot_sync(0xffffffffu, row != nullptr);          // (lanes 0-7: the eight rows)
-                here = next;
-                next = place(j + 2);
+                advance(j);
             };
-            if (tiles) copy(0);
-            for (uint32_t j = 0; j < tiles; ++j) {
-                const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
-                copies_wait<0>();
+            __half2 ratio[4];                               // of scales and unit
+            auto show = [&](uint32_t j) {                   // tile j is there: what softmax wants to know of its rows, then the matrix unit may begin
+                const uint32_t b = j & 1u;
+                const float s[4] = {scales.x, scales.y, scales.z, scales.w};
+                const uint32_t unit = s[0] != 0.f || s[1] != 0.f || s[2] != 0.f || s[3] != 0.f ? code_unit(s) : 0u;
+                const float inverse = __uint_as_float((254u << 23) - (unit & 0x7F800000u));
+#pragma unroll
+                for (int g = 0; g < 4; ++g)                 // (NaN where one is no number)
+                    ratio[g] = __half2half2(__float2half_rn(unit < 0x7F800000u ? s[g] * inverse : __uint_as_float(0x7FC00000u)));
+                reinterpret_cast<float*>(shared + L::AT_SCALES)[(4 * b + sub) * TILE + line] = sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
+                if (sub == 0) units[b * TILE] = (uint8_t)(unit >> 23);
+                put_top(b, __uint_as_float(unit));
+                put_seen(b, group_warp, row);
+                announce(b, 0);
+            };
+            uint4 body[16];
+            auto take = [&](uint32_t j) {
+                const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
                 uint32_t w[8][4];
 #pragma unroll
                 for (uint32_t u = 0; u < 8; ++u)
                     asm volatile("ld.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3])
                                  : "r"(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub)));
-                const float s[4] = {s_next[0], s_next[1], s_next[2], s_next[3]};
-                const uint32_t unit = s[0] != 0.f || s[1] != 0.f || s[2] != 0.f || s[3] != 0.f ? code_unit(s) : 0u;
-                reinterpret_cast<float*>(shared + L::AT_SCALES)[(4 * b + sub) * TILE + line] = sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
-                if (sub == 0) units[b * TILE] = (uint8_t)(unit >> 23);
-                put_top(b, __uint_as_float(unit));
-                if (lane == 0) shared[L::AT_SEEN + 8 * b + warp - SOFTMAX_WARPS] = (uint8_t)seen_next;
-                announce(b, 0);
-                if (j + 1 < tiles) {                        // into the other place, as soon as the scores of the tile there are through
-                    if (j >= 1 && !__all_sync(0xffffffffu, wait(bars + CODES_READ + 8 * (b ^ 1u), (j - 1) >> 1 & 1u, misc))) break;
-                    copy(j + 1);
-                }
-                // (converted while the last tile's values are still read)
-                const float inverse = __uint_as_float((254u << 23) - (unit & 0x7F800000u));
-                uint4 body[16];
 #pragma unroll
                 for (uint32_t u = 0; u < 8; ++u) {
-                    // ratio of scale and unit as fp16; NaN where one is no number
-                    const __half2 ratio = __half2half2(__float2half_rn(unit < 0x7F800000u ? s[u / 2] * inverse : __uint_as_float(0x7FC00000u)));
                     uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        x[i] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[u][i / 2] >> (i % 2 * 16)), __NV_E4M3)), ratio));
+                        x[i] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[u][i / 2] >> (i % 2 * 16)), __NV_E4M3)), ratio[u / 2]));
                     body[2 * u] = make_uint4(x[0], x[1], x[2], x[3]);
                     body[2 * u + 1] = make_uint4(x[4], x[5], x[6], x[7]);
                 }
-                if (j >= 1 && !free(j - 1)) break;
+            };
+            if (tiles) {
+                copy(0);
+                copies_wait<0>();
+                show(0);
+                take(0);
+            }
+            for (uint32_t j = 0; j < tiles; ++j) {
+                if (j + 1 < tiles) {                        // into the other place, as soon as the scores of the tile there are through
+                    if (j >= 1 && !passed(CODES_READ, j - 1)) break;
+                    copy(j + 1);
+                    copies_wait<0>();
+                    if (j >= 1 && !passed(WEIGHTS, j - 1)) break;                // (who reads the scales of the tile before is through)
+                    show(j + 1);
+                }
+                if (j >= 1 && !passed(FREE, j - 1)) break;
                 // numbers 64 u + 16 sub ..
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) put16(place_of(base + L::AT_VALUES + i / 2 * PIECE, line, 2 * sub + i % 2), body[i]);
                 fence_for_matrix_unit();
                 arrive(bars + VALUES, lane);
+                if (j + 1 < tiles) take(j + 1);
             }
             copies_wait<0>();
         } else {
@@ -697,14 +734,13 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     }
                     if (!__all_sync(0xffffffffu, wait(bar, parity, misc))) break;
                 }
-                const uint8_t* row = row_of(here);
+                const uint8_t* row = row_of(here[0]);
                 const uint8_t* from = row ? row : p.buffer;                      // (a masked row's bytes are zeros, nothing is read)
-                put_seen(b, row);
+                put_seen(b, warp & 7u, row);
 #pragma unroll
                 for (uint32_t u = 0; u < 2 * BODY + 2; ++u) copy16(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub), from + 16 * (4 * u + sub), !row);
                 copies_close();
-                here = next;
-                next = place(j + 2);
+                advance(j);
                 if (there < j) {                                                 // the tile before this one is announced when it is there
                     copies_wait<1>();
                     while (there < j) announce_both(there++);
