@@ -637,12 +637,24 @@ _APPEND = struct.Struct("=4I3Q2Q2Q4QQ5Q")
 _ATTEND = struct.Struct("=6I5Q3QQ3QQ2f6Q")
 _ROWS_CALL = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p)
 _append_fn = _attend_fn = None
+_tensor_calls = False                                # the extension module that makes these calls (csrc/tensor_calls.cpp), where it loads
 
 
 def _rows_functions():
-    global _append_fn, _attend_fn
+    global _append_fn, _attend_fn, _tensor_calls
     lib = load_library()
+    try:
+        from . import _tensor_calls as module
+    except ImportError:                              # not built, or for another torch: the same calls are marshalled below
+        pass
+    else:
+        module.set_library(_address_of(lib.avsg_append), _address_of(lib.avsg_attend), _address_of(lib.avsg_row_bytes))
+        _tensor_calls = module
     _append_fn, _attend_fn = _ROWS_CALL(_address_of(lib.avsg_append)), _ROWS_CALL(_address_of(lib.avsg_attend))
+
+
+def _stream_number(stream):
+    return stream if stream is None or type(stream) is int else _stream_handle(stream) or 0
 
 
 def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[Rope] = None, rows=None, row_stride=None, kv_rows=None,
@@ -657,6 +669,14 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     import torch
     if _append_fn is None:
         _rows_functions()
+    if _tensor_calls and row_stride is None and kv_rows is None:
+        done = _tensor_calls.append(
+            None if _ctx is None else _ctx._h.value, _tables, latent, rope_part, positions, kv, row_format, None if rope is None else rope.address,
+            rows, bool(want_values), values, None if status is None else _addr(status), _stream_number(stream))
+        if done is not NotImplemented:
+            if done[0] != OK:
+                _check(done[0], "avsg_append")
+            return done[1]
     device, dtype, shape = latent.get_device(), latent.dtype, latent.shape
     if device < 0 or len(shape) != 3 or shape[2] != LATENT_DIMS or latent.stride(2) != 1:
         raise AvsgError(EINVAL, "append: latent is a CUDA tensor [n, n_tokens, 512] with its last numbers side by side")
@@ -718,6 +738,14 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     import torch
     if _attend_fn is None:
         _rows_functions()
+    if _tensor_calls:
+        done = _tensor_calls.attend(
+            None if _ctx is None else _ctx._h.value, _tables, q, buffer, slots, row_format, scale, out, lse, bool(want_lse), softcap, ids,
+            positions, spans, slopes, None if rope is None else rope.address, None if status is None else _addr(status), _stream_number(stream))
+        if done is not NotImplemented:
+            if done[0] != OK:
+                _check(done[0], "avsg_attend")
+            return done[1]
     device, shape, bf16, int32 = q.get_device(), q.shape, torch.bfloat16, torch.int32
     if device < 0 or q.dtype is not bf16 or len(shape) != 4 or shape[3] != LATENT_DIMS + ROPE_DIMS or q.stride(3) != 1:
         raise AvsgError(EINVAL, "attend: q is a bf16 CUDA tensor [n, n_tokens, heads, 576] with its last numbers side by side")

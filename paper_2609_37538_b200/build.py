@@ -1,4 +1,4 @@
-"""Compiles csrc/*.cu into libavsg.so with nvcc for sm_100a, and the binding's extension module with g++ (both in-tree)."""
+"""Compiles csrc/*.cu into libavsg.so with nvcc for sm_100a, and the binding's extension modules with g++ (all in-tree)."""
 import glob
 import os
 import subprocess
@@ -11,6 +11,8 @@ INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libavsg.so")
 CALLS_SOURCE = os.path.join(CSRC, "python_calls.cpp")
 CALLS = os.path.join(_HERE, "_python_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # (of this Python)
+TENSOR_CALLS_SOURCE = os.path.join(CSRC, "tensor_calls.cpp")
+TENSOR_CALLS = os.path.join(_HERE, "_tensor_calls" + sysconfig.get_config_var("EXT_SUFFIX"))      # (of this Python and this torch)
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -41,14 +43,32 @@ def build_calls(force: bool = False):
     return CALLS
 
 
+def build_tensor_calls(force: bool = False):
+    """The extension module that makes the calls with torch's tensors, rebuilt when a source is newer."""
+    deps = [TENSOR_CALLS_SOURCE] + glob.glob(os.path.join(INCLUDE, "*.h"))
+    if force or not os.path.exists(TENSOR_CALLS) or any(os.path.getmtime(d) > os.path.getmtime(TENSOR_CALLS) for d in deps):
+        import torch
+        root = os.path.dirname(torch.__file__)
+        headers = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), "/usr/local/cuda/include"]
+        tmp = TENSOR_CALLS + ".tmp.%d" % os.getpid()
+        subprocess.check_call([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden",
+                               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                               "-I", sysconfig.get_paths()["include"], "-I", INCLUDE] + [x for h in headers for x in ("-isystem", h)] +
+                              ["-o", tmp, TENSOR_CALLS_SOURCE, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                               "-ltorch_python"])
+        os.replace(tmp, TENSOR_CALLS)
+    return TENSOR_CALLS
+
+
 def build_library(force: bool = False, verbose: bool = False):
-    """Returns the path of libavsg.so, rebuilding it (and the extension module) when a source is newer.  The library needs no
-    Python; where the module cannot be built (no C++ compiler, no Python.h) the binding goes without it."""
+    """Returns the path of libavsg.so, rebuilding it (and the extension modules) when a source is newer.  The library needs no
+    Python; where a module cannot be built (no C++ compiler, no Python.h, no torch) the binding goes without it."""
     lib = _build_library(force, verbose)
-    try:
-        build_calls(force)
-    except (OSError, subprocess.CalledProcessError) as e:
-        warnings.warn("the binding's extension module was not built (%s): calls are marshalled by ctypes" % e)
+    for build in (build_calls, build_tensor_calls):
+        try:
+            build(force)
+        except (ImportError, OSError, subprocess.CalledProcessError) as e:
+            warnings.warn("an extension module of the binding was not built (%s): calls are marshalled by ctypes" % e)
     return lib
 
 
