@@ -34,7 +34,6 @@ namespace avsg {
 namespace {
 
 constexpr uint32_t TILE = 64, GROUP = 64;                   // rows of a tile, most heads of a block
-constexpr uint32_t SOFTMAX_WARPS = 8, ROW_WARPS = 8, WARPS = SOFTMAX_WARPS + ROW_WARPS + 1, THREADS = 32 * WARPS;
 constexpr uint32_t PIECE = 64 * 128;                        // 64 lines of 64 numbers
 constexpr uint32_t BODY = LATENT / 64;                      // pieces of 64 16-bit numbers a line
 constexpr uint32_t MAX_CLUSTER = 8;
@@ -45,7 +44,8 @@ template <uint32_t FORMAT>
 struct Layout {
     static constexpr bool HALF = FORMAT != AVSG_ROW_BF16;                       // fp16 weights and values
     static constexpr bool CODES = FORMAT == AVSG_ROW_FP8;                       // scores from e4m3 codes
-    static constexpr uint32_t TURNS = FORMAT == AVSG_ROW_FP4 ? 2 : 1;           // groups of row warps that take tiles in turn
+    static constexpr uint32_t SOFTMAX_WARPS = CODES ? 16 : 8, SHARES = SOFTMAX_WARPS / 4, EACH = TILE / SHARES;        // rows of a tile to each
+    static constexpr uint32_t ROW_WARPS = 8, WARPS = SOFTMAX_WARPS + ROW_WARPS + 1, THREADS = 32 * WARPS;
     static constexpr uint32_t STEPS = CODES ? 3 : 1;                            // of a tile's S: two latent sums, two, the rotated one; or all at once
     static constexpr uint32_t PARTS = CODES ? 3 : 2;                            // in which its products are issued
     static constexpr uint32_t ROPE_PIECE = CODES ? BODY / 2 : BODY;             // of a tile: the rotated numbers (behind 128 or 64 numbers a line)
@@ -54,15 +54,15 @@ struct Layout {
     // which are overwritten as soon as scores are there; else they take that of the tile's rotated numbers, read by then.
     static constexpr uint32_t AT_Q = 0, AT_TILES = (BODY + 1) * PIECE, AT_VALUES = AT_TILES + 2 * TILE_BYTES, AT_WEIGHTS = AT_VALUES + (CODES ? BODY * PIECE : 0);
     static constexpr uint32_t AT_SCALES = AT_WEIGHTS + (CODES ? PIECE : 0), AT_UNITS = AT_SCALES + (CODES ? 2 * 4 * TILE * 4 : 0);
-    static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE,              // (units of the tiles' rows: powers of two, by their exponents)
- AT_TOPS = AT_SEEN + 16, TOPS = ROW_WARPS / TURNS, AT_ALPHA = AT_TOPS + 2 * TOPS * 4, AT_PEAK = AT_ALPHA + GROUP * 4;
-    static constexpr uint32_t AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 80;
+    // (units of the tiles' rows are powers of two, by their exponents; 16 bits of who is seen)
+    static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE, AT_TOPS = AT_SEEN + 16, TOPS = 8, AT_ALPHA = AT_TOPS + 2 * TOPS * 4;
+    static constexpr uint32_t AT_PEAK = AT_ALPHA + GROUP * 4, AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 128;
     static constexpr uint32_t AT_UNIT = AT_ALPHA;                               // the queries' units, until the softmax warps have read them
-    // once all products are through: O in 32 bits [heads][512], the blocks' shares in it, the running maxima and the sums of two halves
+    // once all products are through: O in 32 bits [heads][512], the blocks' shares in it, the running maxima and the sums of each share of a tile's rows
     static constexpr uint32_t AT_OUT = AT_TILES, AT_SHARE = AT_OUT + GROUP * LATENT * 4, AT_MOST = AT_SHARE + MAX_CLUSTER * GROUP * 4, AT_SUM = AT_MOST + GROUP * 4;
-    static_assert(AT_SUM + 2 * GROUP * 4 <= AT_SCALES && TOTAL <= 232448, "");
+    static_assert(AT_SUM + SHARES * GROUP * 4 <= AT_SCALES && TOTAL <= 232448, "");
 };
-constexpr uint32_t SHARED_MOST = Layout<AVSG_ROW_FP8>::TOTAL;
+constexpr uint32_t SHARED_MOST = Layout<AVSG_ROW_FP8>::TOTAL, MAX_WARPS = 25;
 
 // Barriers, by their place: half of a tile laid out (two of two tiles); tile read (2); step of S there, read (2 each); weights there (2); values
 // there; queries there; codes read by the matrix unit (2).
@@ -81,10 +81,10 @@ constexpr long long WAIT_CLOCKS = 1ll << 29;                // about 0.3 s: long
 
 struct Misc {
     uint32_t tmem, failed;
-    int32_t last[WARPS];
+    int32_t last[MAX_WARPS];
     float unit;                         // what O's weights are multiples of
 };
-static_assert(sizeof(Misc) <= 80, "");
+static_assert(sizeof(Misc) <= 128, "");
 
 // Waits, bounded: false (and the block's other waits end too) if nothing came.  All lanes of a warp look together, in one instruction: 20
 // clocks where the phase is over.  (One lane looking for the others: 400, coming together again.)
@@ -106,6 +106,9 @@ __device__ __forceinline__ void arrive(uint32_t bar, uint32_t lane)
     if (lane == 0) barrier_arrive(bar);
 }
 
+// The bits of a float as an integer of the same order, and back.
+__device__ __forceinline__ int in_order(int bits) { return bits ^ (bits >> 31 & 0x7FFFFFFF); }
+
 __device__ __forceinline__ uint4 zeros() { return make_uint4(0u, 0u, 0u, 0u); }
 
 __device__ __forceinline__ uint32_t place_of(uint32_t piece, uint32_t line, uint32_t unit) { return piece + line * 128u + ((unit ^ (line & 7u)) << 4); }
@@ -124,19 +127,13 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// What a lane of a row warp has of a row in 4 bits: every fourth 16-byte unit, and all scales.
-struct RowPart { uint4 body[4], rope[2], scales; };
+// What a lane of a row warp has of eight rows in 4 bits: 16 bytes each of the codes' first and second half of row lane / 8 and of the one 4
+// further on; of the rotated numbers likewise; all scales of row lane % 8 (lanes 0-7).  (Eight lanes read 128 bytes of a row side by side:
+// eight rows' 16 bytes would be eight lookups of the cache for one, which bound the kernel.)
+struct RowPart { uint4 body[2][2], rope[2], scales; };
 
-__device__ __forceinline__ void get_row(RowPart& v, const uint8_t* row, uint32_t sub)
-{
-    const uint4* at = reinterpret_cast<const uint4*>(row);
-    // (masked: zeros, so that nothing of it reaches a sum)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.body[i] = row ? __ldg(at + 4 * i + sub) : zeros();
-    v.scales = row ? __ldg(at + 16) : zeros();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) v.rope[i] = row ? __ldg(at + 17 + 4 * i + sub) : zeros();
-}
+// (masked: zeros, so that nothing of it reaches a sum)
+__device__ __forceinline__ uint4 unit_at(const uint8_t* row, uint32_t unit) { return row ? __ldg(reinterpret_cast<const uint4*>(row) + unit) : zeros(); }
 
 // The unit that a 4-bit row's numbers are in: 2^-13 of its largest scale, so that they reach 6 x 8192 = 49152.
 __device__ __forceinline__ uint32_t nibble_unit(uint4 scales)
@@ -147,16 +144,16 @@ __device__ __forceinline__ uint32_t nibble_unit(uint4 scales)
     return (uint32_t)max((int)most - 13, (int)(LEAST_UNIT >> 23));
 }
 
-// Lays half of a lane's part of such a row out as line `line` of a tile, as fp16: 32 numbers go to units 4 (sub % 2) .. of piece 2 i + sub / 2.  The eight
-// lanes of a store's phase have the eight lines of a piece: no two share a bank.
-__device__ __forceinline__ void put_half(const RowPart& v, int half, uint32_t tile, uint32_t line, uint32_t sub)
+// Lays the lane's 16 bytes of half c of row i (of those above) out as fp16 in line `line` of a tile: 32 numbers go to four units of a piece, in
+// another order for each two lanes, so that the eight lanes of a store's phase, which have one line, share no bank.  unit and scales are of that row.
+__device__ __forceinline__ void put_codes(uint4 body, int c, int unit, uint32_t scales, uint32_t tile, uint32_t line, uint32_t lane)
 {
-    const uint32_t s[4] = {v.scales.x, v.scales.y, v.scales.z, v.scales.w};
-    const int unit = (int)nibble_unit(v.scales);
-#pragma unroll
-    for (int i = 2 * half; i < 2 * half + 2; ++i) {
-        const uint32_t w[4] = {v.body[i].x, v.body[i].y, v.body[i].z, v.body[i].w}, piece = tile + (2 * i + sub / 2) * PIECE;
-        const uint32_t e = s[i] >> (8 * sub) & 255u;
+    const uint32_t turn = lane / 2u & 3u, piece = tile + (4u * c + turn) * PIECE;
+    uint32_t w[4] = {body.x, body.y, body.z, body.w};
+    if (turn & 1u) { const uint32_t x = w[0]; w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = x; }
+    if (turn & 2u) { uint32_t x = w[0]; w[0] = w[2]; w[2] = x; x = w[1]; w[1] = w[3]; w[3] = x; }
+    {
+        const uint32_t e = scales >> (8u * (lane & 3u)) & 255u;
         const int power = (int)e - unit;                                        // scale / unit is 2^power, power <= 13
         if (power >= -13 && e != 255u) {
             // The upper bytes of 0, .5, 1, 1.5 and 2, 3, 4, 6 times 2^power as fp16 (the lower are zero), looked up by a code's last three bits, four
@@ -167,7 +164,7 @@ __device__ __forceinline__ void put_half(const RowPart& v, int half, uint32_t ti
                 const uint32_t even = w[u] << 4;
                 const uint32_t a = __byte_perm(small, large, w[u] & 0x7777u) | (__byte_perm(even, w[u], 0xD9C8) & 0x80808080u);
                 const uint32_t b = __byte_perm(small, large, w[u] >> 16 & 0x7777u) | (__byte_perm(even, w[u], 0xFBEA) & 0x80808080u);
-                put16(place_of(piece, line, 4 * (sub % 2) + u),
+                put16(place_of(piece, line, 4u * (lane & 1u) + (turn + u & 3u)),
                       make_uint4(__byte_perm(a, 0, 0x1404), __byte_perm(a, 0, 0x3424), __byte_perm(b, 0, 0x1404), __byte_perm(b, 0, 0x3424)));
             }
         } else {                                                                // below fp16's full digits, or no number
@@ -177,7 +174,7 @@ __device__ __forceinline__ void put_half(const RowPart& v, int half, uint32_t ti
                 uint32_t x[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = bits(__hmul2(e2m1_pair(w[u] >> (8 * j) & 255u), *reinterpret_cast<const __half2*>(&ratio)));
-                put16(place_of(piece, line, 4 * (sub % 2) + u), make_uint4(x[0], x[1], x[2], x[3]));
+                put16(place_of(piece, line, 4u * (lane & 1u) + (turn + u & 3u)), make_uint4(x[0], x[1], x[2], x[3]));
             }
         }
     }
@@ -202,9 +199,11 @@ __device__ __forceinline__ void split(__half2 x, uint32_t& high, uint32_t& low)
 }  // namespace
 
 template <uint32_t FORMAT, bool SHAPED>
-__global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_constant__ AttendParams p)
+__global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel(const __grid_constant__ AttendParams p)
 {
     using L = Layout<FORMAT>;
+    constexpr uint32_t SOFTMAX_WARPS = L::SOFTMAX_WARPS, ROW_WARPS = L::ROW_WARPS, WARPS = L::WARPS, THREADS = L::THREADS, SHARES = L::SHARES;
+    static_assert(WARPS <= MAX_WARPS, "");
     extern __shared__ __align__(1024) uint8_t shared[];
     const uint32_t base = shared_address(shared), bars = base + L::AT_BARS;
     Misc* misc = reinterpret_cast<Misc*>(shared + L::AT_MISC);
@@ -215,12 +214,12 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
     const uint32_t table = item / p.n_tokens, token = item - table * p.n_tokens;
     const uint32_t first_head = group * p.group_heads, heads = min(p.group_heads, p.heads - first_head);
     const uint32_t columns = (heads + 15u) & ~15u;
-    // Head h is line 16 (h / in_quarter) + h % in_quarter of S: a quarter of TMEM's lanes, and two softmax warps, have in_quarter heads.
+    // Head h is line 16 (h / in_quarter) + h % in_quarter of S: a quarter of TMEM's lanes, and SHARES softmax warps, have in_quarter heads.
     const uint32_t in_quarter = (heads + 3u) / 4u, quarters = (heads + in_quarter - 1u) / in_quarter;
     const int32_t* slots = p.slots + (uint64_t)item * p.topk;
     const int32_t* ids = p.ids ? p.ids + (uint64_t)item * p.topk : nullptr;
 
-    // Queries are asked for first: warp w has heads w, w + 17, ...
+    // Queries are asked for first: warp w has heads w, w + WARPS, ...
     constexpr uint32_t MINE = (GROUP + WARPS - 1) / WARPS;
     const uint32_t first = p.rope.halves ? lane : 2u * lane, second = p.rope.halves ? lane + 32u : 2u * lane + 1u;
     uint4 q[MINE][2];
@@ -239,42 +238,47 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             }
         }
     }
-    // A row warp's first slots too, for its first two tiles: of a line a lane, or of two where warps take turns.
-    const uint32_t first_tile = L::TURNS > 1 ? (warp - SOFTMAX_WARPS) / 4u & 1u : 0u;
-    const uint32_t line = L::TURNS > 1 ? (warp & 3u) * 16u + lane % 8u : (warp & 7u) * 8u + lane % 8u;
+    // A row warp's first rows too: a lane has every fourth 16-byte unit of one of its warp's eight lines.
+    const uint32_t sub = lane / 8u, group_warp = (warp - SOFTMAX_WARPS) & 7u, line = group_warp * 8u + lane % 8u;
+    const uint8_t* rows = p.buffer + (uint64_t)(p.mapped ? p.table_id[table] : table) * p.table_stride;
+    int32_t begin = INT32_MIN, end = INT32_MAX;
     struct Place { int32_t slot, id; };
-    auto place_at = [&](uint32_t j, uint32_t at) -> Place {
+    auto place = [&](uint32_t j) -> Place {                 // the slot (and id) of tile j's line
         Place to = {-1, 0};
-        const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + at;
+        const uint64_t k = (uint64_t)(rank + j * p.cluster) * TILE + line;
         if (k < p.topk) {
             to.slot = __ldg(slots + k);
             if (p.spans) to.id = __ldg(ids + k);
         }
         return to;
     };
-    Place here[2] = {{-1, 0}, {-1, 0}}, next[2] = {{-1, 0}, {-1, 0}};
+    auto row_of = [&](Place to) -> const uint8_t* {         // where its row is
+        if (to.slot < 0 || (p.spans && (to.id < begin || to.id >= end))) return nullptr;
+        if ((uint32_t)to.slot >= p.rows) { if (p.status) atomicOr(p.status, ST_BAD_SLOT); return nullptr; }
+        return rows + (uint64_t)to.slot * p.row_stride;
+    };
+    Place here = {-1, 0}, next = {-1, 0};                   // of the next tile whose rows are asked for, and the one behind
     if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS) {
-#pragma unroll
-        for (uint32_t i = 0; i < L::TURNS; ++i) {
-            here[i] = place_at(first_tile, line + 8u * i);
-            next[i] = place_at(first_tile + L::TURNS, line + 8u * i);
-        }
+        if (p.spans) { begin = p.spans[2 * item]; end = p.spans[2 * item + 1]; }
+        here = place(0);
+        next = place(1);
     }
     // The selection's last position: what is behind it (padding) costs nothing.
     int32_t last = -1;
     for (uint32_t k = threadIdx.x; k < p.topk; k += THREADS) if (slots[k] >= 0) last = (int32_t)k;
     last = __reduce_max_sync(0xffffffffu, last);
     if (lane == 0) misc->last[warp] = last;
+    if (threadIdx.x < GROUP) reinterpret_cast<int*>(shared + L::AT_PEAK)[threadIdx.x] = in_order(__float_as_int(-INFINITY));
     if (threadIdx.x == 0) {
         misc->failed = 0;
-        for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, ROW_WARPS / L::TURNS);
+        for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, 8);
         for (uint32_t i = 0; i < 2; ++i) {
             barrier_init(bars + FREE + 8 * i, 1);
             barrier_init(bars + SUM_FULL + 8 * i, 1);
-            barrier_init(bars + SUM_FREE + 8 * i, 2 * quarters);
+            barrier_init(bars + SUM_FREE + 8 * i, SHARES * quarters);
             barrier_init(bars + WEIGHTS + 8 * i, SOFTMAX_WARPS);
         }
-        barrier_init(bars + VALUES, ROW_WARPS);
+        barrier_init(bars + VALUES, 8);
         for (uint32_t i = 0; i < 2; ++i) barrier_init(bars + CODES_READ + 8 * i, 1);
         barrier_init(bars + QUERIES, WARPS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -288,6 +292,36 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
     for (uint32_t w = 0; w < WARPS; ++w) last = max(last, misc->last[w]);
     const uint32_t all_tiles = (uint32_t)(last + 1 + (int32_t)TILE - 1) / TILE;
     const uint32_t tiles = all_tiles > rank ? (all_tiles - rank + p.cluster - 1) / p.cluster : 0u;       // rank, rank + cluster, ...
+
+    const uint8_t* row = nullptr;                           // of lane % 8 of a warp's eight
+    auto row_at = [&](const uint8_t* row, uint32_t from) {
+        return reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), (int)from));
+    };
+    float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);        // (e4m3 rows, lanes 0-7)
+    // The rows of tile j, copied as they are.  A masked row's bytes are zeros, nothing is read.
+    auto fetch = [&](uint32_t j) {
+        const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
+        row = row_of(here);
+        here = next;
+        next = j + 2 < tiles ? place(j + 2) : Place{-1, 0};
+        // Eight lanes copy 128 bytes of a row side by side.  (Eight rows' 16 bytes: eight lookups of the cache for one, which bound the kernel.)
+        const uint8_t* from[2] = {row_at(row, lane / 8u), row_at(row, 4u + lane / 8u)};
+        if (L::CODES && lane < 8u) scales = row ? __ldg(reinterpret_cast<const float4*>(row + LATENT)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (uint32_t u = 0; u <= L::ROPE_PIECE; ++u)
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+                copy16(place_of(tile + u * PIECE, group_warp * 8u + 4u * i + lane / 8u, lane % 8u),
+                       (from[i] ? from[i] : p.buffer) + (u < L::ROPE_PIECE ? 128 * u : row_bytes_of(FORMAT) - 2 * ROPE) + 16u * (lane % 8u), !from[i]);
+        copies_close();
+    };
+    if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS && tiles) {
+        if constexpr (FORMAT == AVSG_ROW_FP4) {             // (registers are for queries now)
+            if (here.slot >= 0 && (uint32_t)here.slot < p.rows) asm volatile("prefetch.global.L2 [%0];" :: "l"(rows + (uint64_t)here.slot * p.row_stride + min(128u * sub, 399u)));
+        } else {
+            fetch(0);
+        }
+    }
 
     // ---- queries ----
     {
@@ -350,8 +384,9 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
     }
 
     if (warp < SOFTMAX_WARPS) {
-        // ---- softmax: a thread has 8 rows' scores of two heads, lines r and r + 8 of its quarter ----
-        const uint32_t quarter = warp & 3u, half = warp >> 2, quad = lane & 3u;
+        // ---- softmax: a thread has COUNT rows' scores of two heads, lines r and r + 8 of its quarter ----
+        constexpr int COUNT = L::EACH / 4;
+        const uint32_t quarter = warp & 3u, share = warp >> 2, quad = lane & 3u;
         const bool busy = quarter < quarters, two = in_quarter > 8u;               // (not two: nobody has a second head)
         uint32_t head[2];
         bool real[2];
@@ -370,29 +405,29 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
         }
         const int32_t position = SHAPED && p.slopes ? p.positions[item] : 0;
         float most[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f}, unit = __uint_as_float(LEAST_UNIT);
-        const uint32_t lanes = tmem + (quarter * 32u << 16), row = 32u * half + 2u * quad;        // (this thread's rows: 8 c + i, c = 0 .. 3, i = 0, 1, from there)
+        const uint32_t lanes = tmem + (quarter * 32u << 16), row = L::EACH * share + 2u * quad;       // (this thread's rows: 8 c + i, i = 0, 1, from there)
         auto outgrown = [](float peak, float most) { return peak > most + LAZY<FORMAT> || (most == -INFINITY && peak > -INFINITY); };
-        auto meet = [] { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); };
+        auto meet = [] { asm volatile("barrier.cta.sync 1, %0;" :: "n"(32 * SOFTMAX_WARPS) : "memory"); };
         auto pair_at = [&](uint32_t at, uint32_t c) { return *reinterpret_cast<const float2*>(shared + at + 4u * (row + 8u * c)); };
         auto unit_of = [&](uint32_t j, uint32_t c) {
             const uint32_t two = *reinterpret_cast<const uint16_t*>(shared + L::AT_UNITS + TILE * (j & 1u) + row + 8u * c);
             return make_float2(__uint_as_float((two & 255u) << 23), __uint_as_float(two >> 8 << 23));
         };
         auto scale_of = [&](uint32_t j, uint32_t g, uint32_t c) { return pair_at(L::AT_SCALES + 4u * TILE * (4u * (j & 1u) + g), c); };
-        float x[2][8];                                      // a tile's scores (log2), complete after its last step
+        float x[2][COUNT];                                    // a tile's scores (log2), complete after its last step
         // Step g of tile j: a sum or two from TMEM.
         auto take = [&](uint32_t j, uint32_t g) {
             if (!busy || j >= tiles) return;
-            const uint32_t step = j * L::STEPS + g, at = lanes + COL_S + 128 * (step % SLOTS) + 32 * half;
+            const uint32_t step = j * L::STEPS + g, at = lanes + COL_S + 128 * (step % SLOTS) + L::EACH * share;
             wait(bars + SUM_FULL + 8 * (step % SLOTS), step / SLOTS & 1u, misc);
             __syncwarp();
             tmem_after_sync();
-            float s[16], t[16];
-            tmem_load_16x32(at, s);
-            if (FORMAT == AVSG_ROW_FP4 || (FORMAT == AVSG_ROW_FP8 && g < 2)) tmem_load_16x32(at + 64, t);
-            float2 u[4], v[4];
+            float s[2 * COUNT], t[2 * COUNT];
+            tmem_load_scores(at, s);
+            if (FORMAT == AVSG_ROW_FP4 || (FORMAT == AVSG_ROW_FP8 && g < 2)) tmem_load_scores(at + 64, t);
+            float2 u[COUNT / 2], v[COUNT / 2];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < COUNT / 2; ++c) {
                 if (L::CODES && g < 2) { u[c] = scale_of(j, 2 * g, c); v[c] = scale_of(j, 2 * g + 1, c); }
                 if (FORMAT == AVSG_ROW_FP4) u[c] = unit_of(j, c);
             }
@@ -400,7 +435,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             tmem_before_sync();
             arrive(bars + SUM_FREE + 8 * (step % SLOTS), lane);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < COUNT / 2; ++c)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (k == 1 && !two) continue;
@@ -416,11 +451,11 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     }
                 }
         };
-        int32_t id[8];                                      // of this thread's rows, where scores have a bias by distance
+        int32_t id[COUNT];                                     // of this thread's rows, where scores have a bias by distance
         auto ask_ids = [&](uint32_t j) {
             if (SHAPED && busy && p.slopes)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
+                for (int c = 0; c < COUNT; ++c) {
                     const uint64_t at = (uint64_t)(rank + j * p.cluster) * TILE + row + 8 * (c / 2) + c % 2;
                     id[c] = at < p.topk ? __ldg(ids + at) : 0;
                 }
@@ -435,7 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             if (busy) {
                 if constexpr (SHAPED) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < COUNT; ++c) {
                         const float away = p.slopes ? (float)(id[c] - position) : 0.f;
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
@@ -446,33 +481,35 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                         }
                     }
                 }
-                const uint32_t seen = *reinterpret_cast<const uint32_t*>(shared + L::AT_SEEN + 8 * b + 4 * half) >> (2u * quad);
-                if ((seen & 0x03030303u) != 0x03030303u) {  // masked ones among this thread's rows
+                const uint32_t seen = (COUNT == 8 ? *reinterpret_cast<const uint32_t*>(shared + L::AT_SEEN + 8 * b + 4 * share)
+                                                  : *reinterpret_cast<const uint16_t*>(shared + L::AT_SEEN + 8 * b + 2 * share)) >> (2u * quad);
+                constexpr uint32_t ALL = COUNT == 8 ? 0x03030303u : 0x0303u;
+                if ((seen & ALL) != ALL) {  // masked ones among this thread's rows
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
+                    for (int c = 0; c < COUNT; ++c)
                         if (!(seen >> (8 * (c / 2) + c % 2) & 1u)) x[0][c] = x[1][c] = -INFINITY;
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (k == 1 && !two) continue;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) peak[k] = fmaxf(peak[k], x[k][c]);
+                    for (int c = 0; c < COUNT; ++c) peak[k] = fmaxf(peak[k], x[k][c]);
                     behind |= real[k] && outgrown(peak[k], most[k]);
                 }
                 if (L::HALF) behind |= reinterpret_cast<const float*>(shared + L::AT_TOPS)[b * L::TOPS + lane % L::TOPS] > unit;
             }
             // Weights would grow beyond their range: the references move, and O is brought to the new ones before it is added to.
             int any;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, 256, q;\n\tselp.s32 %0, 1, 0, p;\n\t}"
-                         : "=r"(any) : "r"((int)behind) : "memory");
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tbarrier.cta.red.or.pred p, 1, %2, q;\n\tselp.s32 %0, 1, 0, p;\n\t}"
+                         : "=r"(any) : "r"((int)behind), "n"(32 * SOFTMAX_WARPS) : "memory");
             if (any) {
-                float* peaks = reinterpret_cast<float*>(shared + L::AT_ALPHA);                // of the first half's rows, then of the second's
+                int* peaks = reinterpret_cast<int*>(shared + L::AT_PEAK);
                 if (busy)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         peak[k] = fmaxf(peak[k], __shfl_xor_sync(0xffffffffu, peak[k], 1));
                         peak[k] = fmaxf(peak[k], __shfl_xor_sync(0xffffffffu, peak[k], 2));
-                        if (real[k] && quad == 0) peaks[half * GROUP + head[k]] = peak[k];
+                        if (real[k] && quad == 0) atomicMax(peaks + head[k], in_order(__float_as_int(peak[k])));
                     }
                 float less = 1.f, keep[2] = {1.f, 1.f};
                 if (L::HALF) {
@@ -490,18 +527,18 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
                         if (real[k]) {
-                            const float to = fmaxf(peaks[head[k]], peaks[GROUP + head[k]]);
+                            const float to = __int_as_float(in_order(peaks[head[k]]));
                             if (outgrown(to, most[k])) {
                                 keep[k] = exp2f(most[k] - to);
                                 most[k] = to;
                                 total[k] *= keep[k];
                             }
+                            if (share == 0 && quad == 0) reinterpret_cast<float*>(shared + L::AT_ALPHA)[head[k]] = keep[k] * less;
                         }
                 meet();
-                if (busy && half == 0 && quad == 0)
+                if (busy && share == 0 && quad == 0)        // (for the next time, which everybody meets before)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) if (real[k]) reinterpret_cast<float*>(shared + L::AT_ALPHA)[head[k]] = keep[k] * less;
-                meet();
+                    for (int k = 0; k < 2; ++k) if (real[k]) peaks[head[k]] = in_order(__float_as_int(-INFINITY));
                 if (j > 0) {
                     wait(bars + FREE + 8 * (b ^ 1u), (j - 1) >> 1 & 1u, misc);
                     __syncwarp();
@@ -510,7 +547,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     // 16 heads at a time, those of which one moved
                     const uint32_t low = __ballot_sync(0xffffffffu, lane < heads && alpha[lane] != 1.f);
                     const uint32_t high = __ballot_sync(0xffffffffu, lane + 32u < heads && alpha[lane + 32u] != 1.f);
-                    for (uint32_t part = 2 * half; part < 2 * half + 2; ++part)
+                    for (uint32_t part = share; part < 4u; part += SHARES)
                         for (uint32_t c = 0; c < columns; c += 16) {
                             if (((c < 32u ? low : high) >> (c % 32u) & 0xFFFFu) == 0) continue;
                             float o[16];
@@ -523,14 +560,14 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     tmem_stored();
                 }
             }
-            uint32_t pair[2][4];                            // weights, two neighbouring rows' to a word
+            uint32_t pair[2][COUNT / 2];                            // weights, two neighbouring rows' to a word
             if (busy) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (k == 1 && !two) continue;
                     const float from = (most[k] == -INFINITY ? 0.f : most[k]) - (L::HALF ? ROOM : 0.f);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < COUNT / 2; ++c) {
                         const float v = exp2f(x[k][2 * c] - from), w = exp2f(x[k][2 * c + 1] - from);
                         total[k] += v + w;
                         pair[k][c] = L::HALF ? bits(__floats2half2_rn(v, w)) : bf16_pair(v, w);
@@ -549,7 +586,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 const uint32_t piece = base + (L::CODES ? L::AT_WEIGHTS : L::AT_TILES + b * L::TILE_BYTES + L::ROPE_PIECE * PIECE);
                 if (L::HALF)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < COUNT / 2; ++c) {
                         const float2 u = unit_of(j, c);
                         const __half2 ratio = __floats2half2_rn(u.x * inverse, u.y * inverse);
 #pragma unroll
@@ -560,7 +597,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 for (int k = 0; k < 2; ++k)
                     if (real[k])
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) put4(place_of(piece, head[k], 4u * half + c) + quad * 4u, pair[k][c]);
+                        for (int c = 0; c < COUNT / 2; ++c) put4(place_of(piece, head[k], COUNT / 2 * share + c) + quad * 4u, pair[k][c]);
             }
             fence_for_matrix_unit();
             tmem_before_sync();
@@ -578,25 +615,14 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 total[k] += __shfl_xor_sync(0xffffffffu, total[k], 1);
                 total[k] += __shfl_xor_sync(0xffffffffu, total[k], 2);
                 if (real[k] && quad == 0) {
-                    if (half == 0) reinterpret_cast<float*>(shared + L::AT_MOST)[head[k]] = most[k] - (L::HALF ? ROOM : 0.f);
-                    reinterpret_cast<float*>(shared + L::AT_SUM)[half * GROUP + head[k]] = total[k];
+                    if (share == 0) reinterpret_cast<float*>(shared + L::AT_MOST)[head[k]] = most[k] - (L::HALF ? ROOM : 0.f);
+                    reinterpret_cast<float*>(shared + L::AT_SUM)[share * GROUP + head[k]] = total[k];
                 }
             }
         }
         if (threadIdx.x == 0) misc->unit = L::HALF ? unit : 1.f;
     } else if (warp < SOFTMAX_WARPS + ROW_WARPS) {
-        // ---- rows: a lane has every fourth 16-byte unit of one of its warp's eight ----
-        const uint32_t sub = lane / 8u;
-        const uint8_t* rows = p.buffer + (uint64_t)(p.mapped ? p.table_id[table] : table) * p.table_stride;
-        int32_t begin = INT32_MIN, end = INT32_MAX;
-        if (p.spans) { begin = p.spans[2 * item]; end = p.spans[2 * item + 1]; }
-        // The slot (and id) of a tile's line, asked for two tiles ahead; where its row is, once it is there.
-        auto place = [&](uint32_t j, uint32_t at) { return j < tiles ? place_at(j, at) : Place{-1, 0}; };
-        auto row_of = [&](Place to) -> const uint8_t* {
-            if (to.slot < 0 || (p.spans && (to.id < begin || to.id >= end))) return nullptr;
-            if ((uint32_t)to.slot >= p.rows) { if (p.status) atomicOr(p.status, ST_BAD_SLOT); return nullptr; }
-            return rows + (uint64_t)to.slot * p.row_stride;
-        };
+        // ---- rows ----
         // (lanes 0-7 speak for eight rows)
         auto put_seen = [&](uint32_t b, uint32_t eight, const uint8_t* row) {
             const uint32_t seen = __ballot_sync(0xffffffffu, row != nullptr);
@@ -606,69 +632,68 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             fence_for_matrix_unit();
             arrive(bars + FULL + 16 * b + 8 * half, lane);
         };
-        const uint32_t group_warp = (warp - SOFTMAX_WARPS) % L::TOPS;
         auto put_top = [&](uint32_t b, float top) {
             top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));                // (not negative; a NaN, too)
             if (lane == 0) reinterpret_cast<float*>(shared + L::AT_TOPS)[b * L::TOPS + group_warp] = top;
         };
         auto passed = [&](uint32_t bar, uint32_t j) { return __all_sync(0xffffffffu, wait(bars + bar + 8 * (j & 1u), j >> 1 & 1u, misc)); };    // of tile j
         uint8_t* units = shared + L::AT_UNITS + line;
-        auto advance = [&](uint32_t j) {                    // the slots of this warp's next tile, and those behind asked for
-#pragma unroll
-            for (uint32_t i = 0; i < L::TURNS; ++i) { here[i] = next[i]; next[i] = place(j + 2 * L::TURNS, line + 8u * i); }
-        };
         if constexpr (FORMAT == AVSG_ROW_FP4) {
-            RowPart part[2];
-            const uint8_t* row[2];
+            // A tile's numbers are in registers; as soon as some are laid out the next tile's are asked for.
+            RowPart part;
+            const uint8_t* from[2];
+            auto advance = [&](uint32_t j) {                // tile j's rows, whose places are known by now
+                row = row_of(here);
+                here = next;
+                next = j + 2 < tiles ? place(j + 2) : Place{-1, 0};
+                for (int i = 0; i < 2; ++i) from[i] = row_at(row, 4u * i + lane / 8u);
+                part.scales = unit_at(lane < 8u ? row : nullptr, 16);
+            };
+            auto ask = [&](int c, int i) { part.body[c][i] = unit_at(from[i], 8u * c + lane % 8u); };
+            auto ask_rope = [&](int i) { part.rope[i] = unit_at(from[i], 17u + lane % 8u); };
+            if (tiles) {
+                advance(0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) { row[i] = row_of(here[i]); get_row(part[i], row[i], sub); }
-            for (uint32_t j = first_tile; j < tiles; j += 2) {
+                for (int c = 0; c < 2; ++c) { ask(c, 0); ask(c, 1); }
+                ask_rope(0); ask_rope(1);
+            }
+            for (uint32_t j = 0; j < tiles; ++j) {
                 const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
-                float unit[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) unit[i] = row[i] ? __uint_as_float(nibble_unit(part[i].scales) << 23) : 0.f;
+                const uint4 scales = part.scales;
+                const uint32_t unit = nibble_unit(scales);
                 if (j >= 2 && !passed(FREE, j - 2)) break;
+                put_seen(b, group_warp, row);
+                if (lane < 8u) units[b * TILE] = (uint8_t)(row ? unit : 0u);
+                put_top(b, __uint_as_float(row && lane < 8u ? unit << 23 : 0u));
+                advance(j + 1);                             // (beyond the last tile: nothing)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    put_seen(b, 2u * group_warp + i, row[i]);
-                    if (sub == 0) units[b * TILE + 8 * i] = (uint8_t)(__float_as_uint(unit[i]) >> 23);
-                }
-                put_top(b, fmaxf(unit[0], unit[1]));
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                for (int c = 0; c < 2; ++c) {
+                    // (codes 32 U .. have scale U: this lane's U is 8 c + lane % 8)
+                    const uint32_t low = c ? scales.z : scales.x, high = c ? scales.w : scales.y;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        put_half(part[i], half, tile, line + 8u * i, sub);
-                        if (half == 1)
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) put16(place_of(tile + L::ROPE_PIECE * PIECE, line + 8u * i, 4 * u + sub), part[i].rope[u]);
+                        const int line = 4 * i + (int)(lane / 8u);
+                        const uint32_t s0 = __shfl_sync(0xffffffffu, low, line), s1 = __shfl_sync(0xffffffffu, high, line);
+                        const int its_unit = (int)__shfl_sync(0xffffffffu, unit, line);
+                        put_codes(part.body[c][i], c, its_unit, lane & 4u ? s1 : s0, tile, group_warp * 8u + line, lane);
+                        ask(c, i);
                     }
-                    announce(b, half);
-                }
-                advance(j);
+                    if (c == 1)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) { row[i] = row_of(here[i]); get_row(part[i], row[i], sub); }
+                        for (int i = 0; i < 2; ++i) {
+                            put16(place_of(tile + L::ROPE_PIECE * PIECE, group_warp * 8u + 4u * i + lane / 8u, lane % 8u), part.rope[i]);
+                            ask_rope(i);
+                        }
+                    announce(b, c);
+                }
             }
         } else if constexpr (L::CODES) {
-            // Codes are copied as they are, a tile ahead; each lane makes values of those that it copied, which nobody else has to wait for.
-            float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);
-            const uint8_t* row = nullptr;
-            auto copy = [&](uint32_t j) {                   // tile j, whose rows `here` has
-                const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
-                row = row_of(here[0]);
-                const uint8_t* from = row ? row : p.buffer;                      // (a masked row's bytes are zeros, nothing is read)
-                scales = row ? __ldg(reinterpret_cast<const float4*>(row + LATENT)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (uint32_t u = 0; u < 8; ++u) copy16(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub), from + 16 * (4 * u + sub), !row);
-#pragma unroll
-                for (uint32_t u = 0; u < 2; ++u) copy16(place_of(tile + L::ROPE_PIECE * PIECE, line, 4 * u + sub), from + row_bytes_of(FORMAT) - 2 * ROPE + 16 * (4 * u + sub), !row);
-                copies_close();
-                advance(j);
-            };
+            // Codes are copied as they are, a tile ahead; each warp makes values of its own eight rows', which nobody else has to wait for.
             __half2 ratio[4];                               // of scales and unit
             auto show = [&](uint32_t j) {                   // tile j is there: what softmax wants to know of its rows, then the matrix unit may begin
                 const uint32_t b = j & 1u;
-                const float s[4] = {scales.x, scales.y, scales.z, scales.w};
+                const float s[4] = {__shfl_sync(0xffffffffu, scales.x, lane % 8u), __shfl_sync(0xffffffffu, scales.y, lane % 8u),
+                                    __shfl_sync(0xffffffffu, scales.z, lane % 8u), __shfl_sync(0xffffffffu, scales.w, lane % 8u)};
                 const uint32_t unit = s[0] != 0.f || s[1] != 0.f || s[2] != 0.f || s[3] != 0.f ? code_unit(s) : 0u;
                 const float inverse = __uint_as_float((254u << 23) - (unit & 0x7F800000u));
 #pragma unroll
@@ -680,52 +705,50 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                 put_seen(b, group_warp, row);
                 announce(b, 0);
             };
-            uint4 body[16];
-            auto take = [&](uint32_t j) {
-                const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
-                uint32_t w[8][4];
-#pragma unroll
-                for (uint32_t u = 0; u < 8; ++u)
-                    asm volatile("ld.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3])
-                                 : "r"(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub)));
-#pragma unroll
-                for (uint32_t u = 0; u < 8; ++u) {
-                    uint32_t x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        x[i] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[u][i / 2] >> (i % 2 * 16)), __NV_E4M3)), ratio[u / 2]));
-                    body[2 * u] = make_uint4(x[0], x[1], x[2], x[3]);
-                    body[2 * u + 1] = make_uint4(x[4], x[5], x[6], x[7]);
-                }
-            };
             if (tiles) {
-                copy(0);
                 copies_wait<0>();
                 show(0);
-                take(0);
             }
             for (uint32_t j = 0; j < tiles; ++j) {
+                __half2 now[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) now[g] = ratio[g];
                 if (j + 1 < tiles) {                        // into the other place, as soon as the scores of the tile there are through
                     if (j >= 1 && !passed(CODES_READ, j - 1)) break;
-                    copy(j + 1);
+                    fetch(j + 1);
                     copies_wait<0>();
                     if (j >= 1 && !passed(WEIGHTS, j - 1)) break;                // (who reads the scales of the tile before is through)
                     show(j + 1);
                 }
                 if (j >= 1 && !passed(FREE, j - 1)) break;
-                // numbers 64 u + 16 sub ..
+                __syncwarp();                               // (all lanes' copies are there)
+                const uint32_t tile = base + L::AT_TILES + (j & 1u) * L::TILE_BYTES;
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) put16(place_of(base + L::AT_VALUES + i / 2 * PIECE, line, 2 * sub + i % 2), body[i]);
+                for (uint32_t u = 0; u < 8; u += 4) {       // numbers 64 u + 16 sub ..
+                    uint32_t w[4][4];
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        asm volatile("ld.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3])
+                                     : "r"(place_of(tile + (u + i) / 2u * PIECE, line, (u + i) % 2u * 4u + sub)));
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        uint32_t x[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            x[k] = bits(__hmul2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i][k / 2] >> (k % 2 * 16)), __NV_E4M3)), now[(u + i) / 2]));
+                        put16(place_of(base + L::AT_VALUES + (u + i) * PIECE, line, 2 * sub), make_uint4(x[0], x[1], x[2], x[3]));
+                        put16(place_of(base + L::AT_VALUES + (u + i) * PIECE, line, 2 * sub + 1), make_uint4(x[4], x[5], x[6], x[7]));
+                    }
+                }
                 fence_for_matrix_unit();
                 arrive(bars + VALUES, lane);
-                if (j + 1 < tiles) take(j + 1);
             }
-            copies_wait<0>();
         } else {
             uint32_t there = 0;                                                  // tiles announced
             auto announce_both = [&](uint32_t tile) { announce(tile & 1u, 0); announce(tile & 1u, 1); };
-            for (uint32_t j = 0; j < tiles; ++j) {
-                const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
+            if (tiles) put_seen(0, group_warp, row);
+            for (uint32_t j = 1; j < tiles; ++j) {
+                const uint32_t b = j & 1u;
                 if (j >= 2) {
                     const uint32_t bar = bars + FREE + 8 * b, parity = (j - 2) >> 1 & 1u;
                     if (there < j && !__all_sync(0xffffffffu, barrier_done(bar, parity))) {
@@ -734,13 +757,8 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
                     }
                     if (!__all_sync(0xffffffffu, wait(bar, parity, misc))) break;
                 }
-                const uint8_t* row = row_of(here[0]);
-                const uint8_t* from = row ? row : p.buffer;                      // (a masked row's bytes are zeros, nothing is read)
-                put_seen(b, warp & 7u, row);
-#pragma unroll
-                for (uint32_t u = 0; u < 2 * BODY + 2; ++u) copy16(place_of(tile + u / 2u * PIECE, line, u % 2u * 4u + sub), from + 16 * (4 * u + sub), !row);
-                copies_close();
-                advance(j);
+                fetch(j);
+                put_seen(b, group_warp, row);
                 if (there < j) {                                                 // the tile before this one is announced when it is there
                     copies_wait<1>();
                     while (there < j) announce_both(there++);
@@ -749,6 +767,7 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             copies_wait<0>();
             if (!misc->failed) while (there < tiles) announce_both(there++);
         }
+        copies_wait<0>();
     } else {
         // ---- products ----
         constexpr Product TYPE = L::HALF ? Product::FP16 : Product::BF16, S_TYPE = L::CODES ? Product::E4M3 : TYPE;
@@ -813,13 +832,11 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
 
     // ---- the block's sums to shared memory, and the cluster's blocks' together ----
     __syncwarp();
-    if (tiles) wait(bars + FREE + 8 * ((tiles - 1) & 1u), (tiles - 1) >> 1 & 1u, misc);
-    __syncwarp();
     tmem_after_sync();
-    if (warp < SOFTMAX_WARPS && tiles) {
+    if (warp < SOFTMAX_WARPS && tiles) {                        // (who have waited for the last product)
         float* out = reinterpret_cast<float*>(shared + L::AT_OUT);
         const uint32_t quarter = warp & 3u;
-        for (uint32_t part = warp / 4u; part < 4u; part += 2)
+        for (uint32_t part = warp / 4u; part < 4u; part += SHARES)
             for (uint32_t c = 0; c < columns; c += 16) {
                 float x[16];
                 tmem_load_32x16(tmem + (quarter * 32u << 16) + COL_OUT + 64 * part + c, x);
@@ -848,7 +865,8 @@ __global__ void __launch_bounds__(THREADS, 1) avsg_attend_kernel(const __grid_co
             sums[c] = units[c] = 0.f;
             if (c < p.cluster) {
                 mosts[c] = load_float(in_block(at_most, c));
-                sums[c] = load_float(in_block(at_sum, c)) + load_float(in_block(at_sum + 4 * GROUP, c));
+                #pragma unroll
+                for (uint32_t i = 0; i < SHARES; ++i) sums[c] += load_float(in_block(at_sum + 4 * GROUP * i, c));
                 units[c] = load_float(in_block(base + L::AT_MISC + offsetof(Misc, unit), c));
             }
         }
@@ -918,10 +936,15 @@ Kernel attend_kernel(uint32_t format, bool shaped)
 constexpr int MAX_DEVICES = 64;
 std::atomic<int> g_active[MAX_DEVICES][4];
 
-cudaLaunchConfig_t config(uint32_t blocks, uint32_t cluster, cudaLaunchAttribute* attr, cudaStream_t stream)
+constexpr uint32_t threads_of(uint32_t format)
+{
+    return format == AVSG_ROW_FP8 ? Layout<AVSG_ROW_FP8>::THREADS : format == AVSG_ROW_FP4 ? Layout<AVSG_ROW_FP4>::THREADS : Layout<AVSG_ROW_BF16>::THREADS;
+}
+
+cudaLaunchConfig_t config(uint32_t format, uint32_t blocks, uint32_t cluster, cudaLaunchAttribute* attr, cudaStream_t stream)
 {
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(blocks); c.blockDim = dim3(THREADS); c.dynamicSmemBytes = SHARED_MOST; c.stream = stream;
+    c.gridDim = dim3(blocks); c.blockDim = dim3(threads_of(format)); c.dynamicSmemBytes = SHARED_MOST; c.stream = stream;
     attr->id = cudaLaunchAttributeClusterDimension;
     attr->val.clusterDim.x = cluster; attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
     c.attrs = attr; c.numAttrs = cluster > 1 ? 1 : 0;
@@ -941,7 +964,7 @@ cudaError_t attend_prepare()
     if (device < 0 || device >= MAX_DEVICES) return cudaSuccess;                        // (then a block per query)
     for (int i = 0; i < 4; ++i) {
         cudaLaunchAttribute attr;
-        const cudaLaunchConfig_t c = config(1u << i, 1u << i, &attr, nullptr);
+        const cudaLaunchConfig_t c = config(AVSG_ROW_FP8, 1u << i, 1u << i, &attr, nullptr);
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(&n, attend_kernel(AVSG_ROW_FP8, false), &c) != cudaSuccess) { cudaGetLastError(); n = 0; }
         g_active[device][i] = n;
@@ -968,7 +991,7 @@ cudaError_t launch_attend(AttendParams& p, uint32_t format, cudaStream_t stream)
     p.groups = (p.heads + p.group_heads - 1) / p.group_heads;
     const uint64_t work = queries * p.groups;
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t c = config((uint32_t)(work * p.cluster), p.cluster, &attr, stream);
+    const cudaLaunchConfig_t c = config(format, (uint32_t)(work * p.cluster), p.cluster, &attr, stream);
     void* args[] = {&p};
     return cudaLaunchKernelExC(&c, reinterpret_cast<const void*>(attend_kernel(format, p.softcap > 0.f || p.slopes)), args);
 }

@@ -57,8 +57,14 @@ __device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// 16 lanes x 32 columns of 32 bits, spread over the warp: x[4 g + i] is row lane / 4 + 8 (i / 2), column 8 g + 2 (lane % 4) + i % 2.
-__device__ __forceinline__ void tmem_load_16x32(uint32_t at, float (&x)[16])
+// 16 lanes x 32 columns (or 16) of 32 bits, spread over the warp: x[4 g + i] is row lane / 4 + 8 (i / 2), column 8 g + 2 (lane % 4) + i % 2.
+__device__ __forceinline__ void tmem_load_scores(uint32_t at, float (&x)[8])
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at));
+}
+__device__ __forceinline__ void tmem_load_scores(uint32_t at, float (&x)[16])
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
