@@ -36,7 +36,6 @@ namespace {
 constexpr uint32_t TILE = 64, GROUP = 64;                   // rows of a tile, most heads of a block
 constexpr uint32_t PIECE = 64 * 128;                        // 64 lines of 64 numbers
 constexpr uint32_t BODY = LATENT / 64;                      // pieces of 64 16-bit numbers a line
-constexpr uint32_t MAX_CLUSTER = 8;
 constexpr uint32_t SLOTS = 2;                               // steps of S under way in TMEM, one or two sums each
 
 // What differs between the formats, and how shared memory is laid out (bytes).
@@ -59,8 +58,8 @@ struct Layout {
     static constexpr uint32_t AT_SEEN = AT_UNITS + 2 * TILE, AT_TOPS = AT_SEEN + 16, TOPS = 8, AT_ALPHA = AT_TOPS + 2 * TOPS * 4;
     static constexpr uint32_t AT_PEAK = AT_ALPHA + GROUP * 4, AT_BARS = AT_PEAK + GROUP * 4, AT_MISC = AT_BARS + 16 * 8, TOTAL = AT_MISC + 128;
     static constexpr uint32_t AT_UNIT = AT_ALPHA;                               // the queries' units, until the softmax warps have read them
-    // once all products are through: O in 32 bits [heads][512], the blocks' shares in it, the running maxima and the sums of each share of a tile's rows
-    static constexpr uint32_t AT_OUT = AT_TILES, AT_SHARE = AT_OUT + GROUP * LATENT * 4, AT_MOST = AT_SHARE + MAX_CLUSTER * GROUP * 4, AT_SUM = AT_MOST + GROUP * 4;
+    // once all products are through: O in 32 bits [heads][512], each head's maximum, sum, unit and their quotient; the running maxima and the sums of each share of a tile's rows
+    static constexpr uint32_t AT_OUT = AT_TILES, AT_STATE = AT_OUT + GROUP * LATENT * 4, AT_MOST = AT_STATE + GROUP * 16, AT_SUM = AT_MOST + GROUP * 4;
     static_assert(AT_SUM + SHARES * GROUP * 4 <= AT_SCALES && TOTAL <= 232448, "");
 };
 constexpr uint32_t SHARED_MOST = Layout<AVSG_ROW_FP8>::TOTAL, MAX_WARPS = 25;
@@ -74,9 +73,8 @@ constexpr uint32_t COL_OUT = 0, COL_S = 256, COLUMNS = 512;
 
 constexpr float LOG2E = 1.4426950408889634f;
 // The maximum that weights refer to lags behind by up to LAZY (log2), so that O is rescaled seldom (bf16 has the range for much more).  fp16
-// weights are 2^ROOM times as large: the largest is 2^4 to 2^15, and all are whole to 2^-25.
-template <uint32_t FORMAT> constexpr float LAZY = Layout<FORMAT>::HALF ? 11.f : 60.f;
-constexpr float ROOM = 4.f;
+// weights are whole to 2^-25 then, the largest being 1 to 2^15.  (2^4 to 2^15: 6% slower with scores that spread over 2^+-12.)
+template <uint32_t FORMAT> constexpr float LAZY = Layout<FORMAT>::HALF ? 15.f : 60.f;
 constexpr uint32_t LEAST_UNIT = 27u << 23;                  // 2^-100: no row's unit is smaller, so that ratios of units stay finite
 constexpr long long WAIT_CLOCKS = 1ll << 29;                // about 0.3 s: longer than any wait that ends
 
@@ -197,6 +195,45 @@ __device__ __forceinline__ void split(__half2 x, uint32_t& high, uint32_t& low)
     low = __nv_cvt_halfraw2_to_fp8x2(__half2_raw(__hsub2(x, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)high, __NV_E4M3)))), __NV_SATFINITE, __NV_E4M3);
 }
 
+__device__ __forceinline__ float logarithm(float most, float total) { return total == 0.f ? -INFINITY : (most + log2f(total)) * 0.6931471805599453f; }
+
+// The sums of a cluster's C blocks, joined: a warp takes a head, or half or a quarter of one, tasks going to the blocks in turn; lanes 0 .. C - 1
+// have the head's numbers of a block each.  What is far away is asked for at once, eight float4 a lane: the time of a task is that of one look.
+template <uint32_t C, uint32_t WARPS>
+__device__ __forceinline__ void join(uint32_t at_state, uint32_t at_out, uint32_t heads, uint32_t rank, uint32_t warp, uint32_t lane, uint8_t* out, uint64_t stride, float* lse)
+{
+    constexpr uint32_t UNITS = 8 / C, TASKS = 4 / UNITS;                        // of 32 float4; of a head
+    for (uint32_t t = warp * C + rank; t < heads * TASKS; t += WARPS * C) {
+        const uint32_t h = t / TASKS, first = t % TASKS * UNITS * 32u + lane;
+        const float4 its = lane < C ? load_float4(in_block(at_state + 16 * h, lane)) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        float4 v[C][UNITS];
+#pragma unroll
+        for (uint32_t c = 0; c < C; ++c)
+#pragma unroll
+            for (uint32_t u = 0; u < UNITS; ++u) v[c][u] = load_float4(in_block(at_out + 16 * (h * (LATENT / 4) + first + 32 * u), c));
+        float most = its.x;
+#pragma unroll
+        for (int m = 1; m < (int)C; m *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
+        const float share = its.y == 0.f ? 0.f : exp2f(its.x - (most == -INFINITY ? 0.f : most));
+        float total = its.y * share;
+#pragma unroll
+        for (int m = 1; m < (int)C; m *= 2) total += __shfl_xor_sync(0xffffffffu, total, m);
+        const float mine = total == 0.f ? 0.f : share * its.z / total;
+        if (lse && first == 0) lse[h] = logarithm(most, total);
+        float w[C];
+#pragma unroll
+        for (uint32_t c = 0; c < C; ++c) w[c] = __shfl_sync(0xffffffffu, mine, (int)c);
+#pragma unroll
+        for (uint32_t u = 0; u < UNITS; ++u) {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t c = 0; c < C; ++c)
+                if (w[c] != 0.f) { x[0] += w[c] * v[c][u].x; x[1] += w[c] * v[c][u].y; x[2] += w[c] * v[c][u].z; x[3] += w[c] * v[c][u].w; }      // (without rows there are no sums)
+            *reinterpret_cast<uint2*>(out + h * stride + 8 * (first + 32 * u)) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+        }
+    }
+}
+
 }  // namespace
 
 template <uint32_t FORMAT, bool SHAPED>
@@ -265,27 +302,30 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
         here = place(first_tile);
         next = place(first_tile + L::TURNS);
     }
+    if (warp == WARPS - 1) {
+        if (lane == 0) {
+            misc->failed = 0;
+            for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, 8);
+            for (uint32_t i = 0; i < 2; ++i) {
+                barrier_init(bars + FREE + 8 * i, 1);
+                barrier_init(bars + SUM_FULL + 8 * i, 1);
+                barrier_init(bars + SUM_FREE + 8 * i, SHARES * quarters);
+                barrier_init(bars + WEIGHTS + 8 * i, SOFTMAX_WARPS);
+            }
+            barrier_init(bars + VALUES, 8);
+            for (uint32_t i = 0; i < 2; ++i) barrier_init(bars + CODES_READ + 8 * i, 1);
+            barrier_init(bars + QUERIES, WARPS);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+        tmem_alloc(base + L::AT_MISC, COLUMNS);
+    }
     // The selection's last position: what is behind it (padding) costs nothing.
     int32_t last = -1;
     for (uint32_t k = threadIdx.x; k < p.topk; k += THREADS) if (slots[k] >= 0) last = (int32_t)k;
     last = __reduce_max_sync(0xffffffffu, last);
     if (lane == 0) misc->last[warp] = last;
     if (threadIdx.x < GROUP) reinterpret_cast<int*>(shared + L::AT_PEAK)[threadIdx.x] = in_order(__float_as_int(-INFINITY));
-    if (threadIdx.x == 0) {
-        misc->failed = 0;
-        for (uint32_t i = 0; i < 4; ++i) barrier_init(bars + FULL + 8 * i, 8);
-        for (uint32_t i = 0; i < 2; ++i) {
-            barrier_init(bars + FREE + 8 * i, 1);
-            barrier_init(bars + SUM_FULL + 8 * i, 1);
-            barrier_init(bars + SUM_FREE + 8 * i, SHARES * quarters);
-            barrier_init(bars + WEIGHTS + 8 * i, SOFTMAX_WARPS);
-        }
-        barrier_init(bars + VALUES, 8);
-        for (uint32_t i = 0; i < 2; ++i) barrier_init(bars + CODES_READ + 8 * i, 1);
-        barrier_init(bars + QUERIES, WARPS);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == WARPS - 1) tmem_alloc(base + L::AT_MISC, COLUMNS);
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
@@ -567,7 +607,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     if (k == 1 && !two) continue;
-                    const float from = (most[k] == -INFINITY ? 0.f : most[k]) - (L::HALF ? ROOM : 0.f);
+                    const float from = (most[k] == -INFINITY ? 0.f : most[k]);
 #pragma unroll
                     for (int c = 0; c < COUNT / 2; ++c) {
                         const float v = exp2f(x[k][2 * c] - from), w = exp2f(x[k][2 * c + 1] - from);
@@ -617,7 +657,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
                 total[k] += __shfl_xor_sync(0xffffffffu, total[k], 1);
                 total[k] += __shfl_xor_sync(0xffffffffu, total[k], 2);
                 if (real[k] && quad == 0) {
-                    if (share == 0) reinterpret_cast<float*>(shared + L::AT_MOST)[head[k]] = most[k] - (L::HALF ? ROOM : 0.f);
+                    if (share == 0) reinterpret_cast<float*>(shared + L::AT_MOST)[head[k]] = most[k];
                     reinterpret_cast<float*>(shared + L::AT_SUM)[share * GROUP + head[k]] = total[k];
                 }
             }
@@ -858,66 +898,34 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
         tmem_after_sync();
         tmem_free(tmem, COLUMNS);
     }
-    if (p.cluster > 1) cluster_sync();
-    float* share = reinterpret_cast<float*>(shared + L::AT_SHARE);
+    // A head's maximum, sum and unit in this block, and the unit's share in the sum.
     if (threadIdx.x < heads) {
-        const uint32_t h = threadIdx.x, at_most = base + L::AT_MOST + 4 * h, at_sum = base + L::AT_SUM + 4 * h;
-        // (all blocks' numbers are asked for before the first is used: they are far away)
-        float mosts[MAX_CLUSTER], sums[MAX_CLUSTER], units[MAX_CLUSTER], most = -INFINITY, total = 0.f;
+        const float* sums = reinterpret_cast<const float*>(shared + L::AT_SUM) + threadIdx.x;
+        float sum = 0.f;
 #pragma unroll
-        for (uint32_t c = 0; c < MAX_CLUSTER; ++c) {
-            mosts[c] = -INFINITY;
-            sums[c] = units[c] = 0.f;
-            if (c < p.cluster) {
-                mosts[c] = load_float(in_block(at_most, c));
-                #pragma unroll
-                for (uint32_t i = 0; i < SHARES; ++i) sums[c] += load_float(in_block(at_sum + 4 * GROUP * i, c));
-                units[c] = load_float(in_block(base + L::AT_MISC + offsetof(Misc, unit), c));
-            }
-        }
-#pragma unroll
-        for (uint32_t c = 0; c < MAX_CLUSTER; ++c) most = fmaxf(most, mosts[c]);
-        const float from = most == -INFINITY ? 0.f : most;
-#pragma unroll
-        for (uint32_t c = 0; c < MAX_CLUSTER; ++c) {
-            mosts[c] = exp2f(mosts[c] - from);
-            total += sums[c] * mosts[c];
-        }
-#pragma unroll
-        for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
-            if (c < p.cluster) share[c * GROUP + h] = sums[c] == 0.f || total == 0.f ? 0.f : mosts[c] * units[c] / total;
-        if (rank == 0 && p.lse)
-            p.lse[(uint64_t)item * p.heads + first_head + h] = total == 0.f ? -INFINITY : (most + log2f(total)) * 0.6931471805599453f;
+        for (uint32_t i = 0; i < SHARES; ++i) sum += sums[i * GROUP];
+        reinterpret_cast<float4*>(shared + L::AT_STATE)[threadIdx.x] = make_float4(reinterpret_cast<const float*>(shared + L::AT_MOST)[threadIdx.x], sum, misc->unit, sum == 0.f ? 0.f : misc->unit / sum);
     }
-    __syncthreads();
+    if (p.cluster > 1) cluster_sync();
+    else __syncthreads();
     uint8_t* out = p.out + table * p.out_stride[0] + token * p.out_stride[1] + first_head * p.out_stride[2];
+    float* lse = p.lse ? p.lse + (uint64_t)item * p.heads + first_head : nullptr;
     if (!misc->failed) {
         if (p.cluster == 1) {
-            const float* from = reinterpret_cast<const float*>(shared + L::AT_OUT);
+            const float4* from = reinterpret_cast<const float4*>(shared + L::AT_OUT);
+            const float4* state = reinterpret_cast<const float4*>(shared + L::AT_STATE);
+            if (lse && threadIdx.x < heads) lse[threadIdx.x] = logarithm(state[threadIdx.x].x, state[threadIdx.x].y);
 #pragma unroll 4
             for (uint32_t u = threadIdx.x; u < heads * (LATENT / 4); u += THREADS) {
                 const uint32_t h = u / (LATENT / 4), d = u % (LATENT / 4);
-                const float w = share[h];
-                const float4 v = w == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : reinterpret_cast<const float4*>(from)[u];      // (without rows there are no sums)
+                const float w = state[h].w;
+                const float4 v = w == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : from[u];                  // (without rows there are no sums)
                 *reinterpret_cast<uint2*>(out + h * p.out_stride[2] + 8 * d) = make_uint2(bf16_pair(w * v.x, w * v.y), bf16_pair(w * v.z, w * v.w));
             }
         } else {
-            for (uint32_t u = rank * THREADS + threadIdx.x; u < heads * (LATENT / 4); u += p.cluster * THREADS) {
-                const uint32_t h = u / (LATENT / 4), d = u % (LATENT / 4);
-                float4 v[MAX_CLUSTER];
-#pragma unroll
-                for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
-                    if (c < p.cluster) v[c] = load_float4(in_block(base + L::AT_OUT + 16 * u, c));
-                float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (uint32_t c = 0; c < MAX_CLUSTER; ++c)
-                    if (c < p.cluster) {
-                        const float w = share[c * GROUP + h];
-                        if (w == 0.f) continue;
-                        x[0] += w * v[c].x; x[1] += w * v[c].y; x[2] += w * v[c].z; x[3] += w * v[c].w;
-                    }
-                *reinterpret_cast<uint2*>(out + h * p.out_stride[2] + 8 * d) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
-            }
+            if (p.cluster == 2) join<2, WARPS>(base + L::AT_STATE, base + L::AT_OUT, heads, rank, warp, lane, out, p.out_stride[2], lse);
+            else if (p.cluster == 4) join<4, WARPS>(base + L::AT_STATE, base + L::AT_OUT, heads, rank, warp, lane, out, p.out_stride[2], lse);
+            else join<8, WARPS>(base + L::AT_STATE, base + L::AT_OUT, heads, rank, warp, lane, out, p.out_stride[2], lse);
         }
     } else if (threadIdx.x == 0 && p.status) {
         atomicOr(p.status, ST_WAIT_TIMEOUT);

@@ -85,7 +85,7 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
     score or cap.  Queries may be two e4m3 numbers, of 4 bits each: off by 2^-17 of the largest one where an element is below 2^-10 of that; or fp16
     in units of 2^-14 of the largest number or finer (off by 2^-38 of it), with 4-bit rows in units of 2^-13 of the row's largest scale, elements
     off by 2^-25 of these.  d bounds the sum of these.  Weights then are off by a factor of exp(+-2 d) and rounded to 16 bits (bf16: 2^-8; fp16
-    rows: three times 2^-11, the row's unit going onto them too); as fp16 they are whole to 2^-25 / 16 of 8 times the unit of the largest row (twice its
+    rows: three times 2^-11, the row's unit going onto them too); as fp16 they are whole to 2^-25 of 8 times the unit of the largest row (twice its
     scale) where the largest weight is 1 or more.  Values of 8-bit rows are fp16, in units of up to 2^-6 of the row's largest scale: off by 2^-11,
     twice (scale and product), and by 2^-25 x 448 of these units where a scale is far below the row's largest.  The result is rounded to bf16 (2^-8).  What is below 2^-126 may count as zero (weights next to the
     largest, results), and so may what is below 2^-100 in rows of 8 and 4 bits."""
@@ -143,7 +143,7 @@ def attend(q, buffer, slots, fmt, scale, softcap=0.0, ids=None, positions=None, 
             less = mass * ((0.0, 5 * 2.0 ** -11, 3 * 2.0 ** -11)[fmt] + (0.0 if fmt else 2.0 ** -8) + torch.expm1(2 * d)[:, None]) + (p @ fine)[:, None]
             less = less + at.numel() * (2.0 ** -126 * k.abs().max() + (2.0 ** -100 if fmt else 0.0))
             if fmt:
-                less = less + 2.0 ** -29 * 16 * unit.max() * code.sum(0) / torch.exp(lse - z.amax(1))[:, None]
+                less = less + 2.0 ** -25 * 16 * unit.max() * code.sum(0) / torch.exp(lse - z.amax(1))[:, None]
             eo.append(less + (o.abs() + less) * 2.0 ** -8 + 2.0 ** -126); el.append(d + lse.abs() * 2.0 ** -22)
     back = lambda v, *tail: torch.stack(v).view(n, T, H, *tail)  # noqa: E731
     return back(outs, LATENT), back(lses), back(eo, LATENT), back(el)
