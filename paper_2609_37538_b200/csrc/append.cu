@@ -42,17 +42,35 @@ __device__ __forceinline__ void sixteen(const uint8_t* p, float (&x)[16])
     for (int i = 0; i < 16; ++i) x[i] = number<TYPE>(reinterpret_cast<const uint8_t*>(w), i);
 }
 
+// Two numbers at a time.
+__device__ __forceinline__ float2 product(float2 a, float2 b)
+{
+    float2 c;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(c)) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+    return c;
+}
+__device__ __forceinline__ float2 sum_of_product(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(d))
+        : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)), "l"(reinterpret_cast<const uint64_t&>(c)));
+    return d;
+}
+
 // x / s such that a later rounding to few bits rounds the exact quotient: cut off towards zero, with the last bit set if anything was
 // cut (a quotient that is not a number of few bits is then none of their midpoints either).  r is 1 / s; q is within one step of the
-// quotient after one correction, and what is left, x - q s, says by its sign on which side of it.
-__device__ __forceinline__ float sticky_quotient(float x, float s, float r)
+// quotient after one correction, and what is left, x - q s, says by its sign on which side of it.  (s is -scale here.)
+__device__ __forceinline__ float2 sticky_quotients(float2 x, float2 s, float2 r)
 {
-    float q = x * r;
-    q = __fmaf_rn(__fmaf_rn(-q, s, x), r, q);
-    const float left = __fmaf_rn(-q, s, x);
-    const uint32_t bits = __float_as_uint(q);
-    const uint32_t cut = (__float_as_uint(left) ^ bits) >> 31;          // the quotient is smaller than q: one step back
-    return copysignf(left == 0.f ? q : __uint_as_float((bits - cut) | 1u), x);        // (a zero keeps its sign)
+    float2 q = product(x, r);
+    q = sum_of_product(sum_of_product(q, s, x), r, q);
+    const float2 left = sum_of_product(q, s, x);
+    auto one = [](float x, float q, float left) {
+        const uint32_t bits = __float_as_uint(q);
+        const uint32_t cut = (__float_as_uint(left) ^ bits) >> 31;      // the quotient is smaller than q: one step back
+        return copysignf(left == 0.f ? q : __uint_as_float((bits - cut) | 1u), x);        // (a zero keeps its sign)
+    };
+    return make_float2(one(x.x, q.x, left.x), one(x.y, q.y, left.y));
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
@@ -82,14 +100,7 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
     const uint32_t table = at / p.n_tokens, token = at - table * p.n_tokens;
     if (table >= p.n_launch) return;
     const int32_t position = p.positions[at];
-    const int32_t row = p.rows ? p.rows[at] : position;
-    if (position < 0 || row < 0) return;
-    if ((uint32_t)row >= p.limit[table]) {
-        if (lane == 0 && p.status) atomicOr(p.status, ST_BAD_ID);
-        return;
-    }
-    uint8_t* out = reinterpret_cast<uint8_t*>(p.base[table]) + (uint64_t)row * p.stride16[table] * 16u;
-    uint8_t* values = p.values ? p.values + (uint64_t)at * (LATENT + ROPE) * 2u : nullptr;
+    // (numbers are asked for before the position is known: padding is rare)
     const uint8_t* latent = p.latent + table * p.latent_stride[0] + token * p.latent_stride[1];
     const uint8_t* part = p.rope_part + table * p.rope_stride[0] + token * p.rope_stride[1];
 
@@ -98,6 +109,14 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
     float a = number<TYPE>(part, first), b = number<TYPE>(part, second);
     float x[16];
     sixteen<TYPE>(latent + lane * (TYPE == AVSG_TYPE_FP32 ? 64u : 32u), x);
+    const int32_t row = p.rows ? p.rows[at] : position;
+    if (position < 0 || row < 0) return;
+    if ((uint32_t)row >= p.limit[table]) {
+        if (lane == 0 && p.status) atomicOr(p.status, ST_BAD_ID);
+        return;
+    }
+    uint8_t* out = reinterpret_cast<uint8_t*>(p.base[table]) + (uint64_t)row * p.stride16[table] * 16u;
+    uint8_t* values = p.values ? p.values + (uint64_t)at * (LATENT + ROPE) * 2u : nullptr;
     if (p.rope.on) {
         float c, s;
         rotation(p.rope, lane, position, c, s);
@@ -134,10 +153,11 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
             __nv_fp8x2_storage_t* c = reinterpret_cast<__nv_fp8x2_storage_t*>(&code);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                c[i] = __nv_cvt_float2_to_fp8x2(make_float2(sticky_quotient(x[2 * i], scale, inverse), sticky_quotient(x[2 * i + 1], scale, inverse)),
+                c[i] = __nv_cvt_float2_to_fp8x2(sticky_quotients(make_float2(x[2 * i], x[2 * i + 1]), make_float2(-scale, -scale), make_float2(inverse, inverse)),
                                                 __NV_SATFINITE, __NV_E4M3);
             reinterpret_cast<uint4*>(out)[lane] = code;
             if (lane % LANES == 0) reinterpret_cast<float*>(out + LATENT)[lane / LANES] = scale;
+            if (values)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(c[i], __NV_E4M3)));
@@ -163,6 +183,7 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
             word |= __shfl_down_sync(0xffffffffu, word, 2) << 16;
             if (lane < 16u && lane % 4u == 0) reinterpret_cast<uint32_t*>(out + LATENT / 2u)[lane / 4u] = word;
             const float scale = odd ? __uint_as_float(0x7FC00000u) : ldexpf(1.f, e);
+            if (values)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float2 v = __half22float2(e2m1_pair((i < 4 ? code.x : code.y) >> (i % 4 * 8) & 255u));
