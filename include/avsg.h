@@ -58,7 +58,7 @@ extern "C" {
 #define AVSG_STATUS_BAD_SEGMENT     0x08u /* Stage Two could not resolve a miss-list entry      */
 #define AVSG_STATUS_BAD_ID          0x10u /* an id >= kv_rows of its table, or >= max_context
                                              with the direct index (taken as padding)          */
-#define AVSG_STATUS_WAIT_TIMEOUT    0x20u /* Stage Two gave up waiting for the Stage One that it follows:
+#define AVSG_STATUS_WAIT_TIMEOUT    0x20u /* (avsg_attend: see there.)  Stage Two gave up waiting for the Stage One that it follows:
                                              rows of THAT call were not copied.  Later calls are
                                              not affected (each takes the hand-over flags down
                                              before its transfer kernel can start)              */
@@ -550,7 +550,16 @@ int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
  * over the positions with a slot >= 0 and, where spans are given, spans[0] <= id < spans[1] (what a query may see: the end
  * alone makes a causal mask, both a document's, an end beyond its own position a prefix's).  A query that sees nothing gets
  * out = 0 and lse = -infinity.  Masked positions are not read, whatever their rows hold; a slot >= the rows of a table is
- * masked too and reported as AVSG_STATUS_BAD_SLOT.
+ * masked too and reported as AVSG_STATUS_BAD_SLOT.  A seen row that holds an infinity or a NaN may make all of its queries' outputs NaN.
+ *
+ * What is rounded: queries and rows are taken as they are (a rotated query to bf16); scores, their maxima and sums are of 32 bits (lse is good
+ * to about 1e-5).  Weights become bf16 with AVSG_ROW_BF16, fp16 with the others, values of AVSG_ROW_FP8 fp16 as well (in units of the row's largest
+ * scale); sums of values are of 32 bits, out is rounded to bf16.  With 8- and 4-bit rows each position's share is rounded to
+ * about 2^-22 of the largest numbers among the rows that the query sees (weighted or not), where the largest weight counts as 1, and what is below
+ * 2^-100 may count as zero.  The same call on the same inputs gives the same bits.
+ *
+ * The kernel's waits are bounded (about 0.3 s, far beyond any that ends): AVSG_STATUS_WAIT_TIMEOUT in the status word means that one of
+ * them ran out, and that the call's outputs are not to be used.
  *
  * ctx may be NULL.  With a context, rows are read from its buffers (buffer NULL), table_ids names the tables, which may repeat, and
  * row_format has to be of the context's row_bytes.  Without one table_ids is NULL and buffer holds n tables of buffer_slots rows

@@ -9,16 +9,24 @@
 // row's, which goes onto score and weight.  e4m3 rows have a scale for every 128 numbers.  A score is computed from the codes as they are
 // (e4m3 x e4m3, a query being two e4m3 numbers: its bf16 has 8 significant bits, two of 4 hold them, down to 2^-17 of the head's largest
 // number), in four sums, onto which the scales go in 32 bits; values are the codes times their scales as fp16, made from the tile's codes beside
-// the first product, with one weight to a row.  (From fp16 rows scores are 4e-4 off; unscaled fp16 rows are exact for both products, but
-// take four sets of weights, one after another through the room that is left: 143 us where this takes @@.)  Other queries become fp16 in
-// units of a power of two of the head's (exact: bf16 has 8 bits, fp16 11), weights fp16 in units of the largest row's.  The rotated 64 numbers are
-// bf16 on both sides and have a sum of their own.
+// the first product, with one weight to a row.  (From fp16 rows scores are 4e-4 off; unscaled fp16 rows are exact for both products, but take four
+// sets of weights, one after another through the room that is left: 143 us where this took 125 at the time.)  Other queries become fp16 in units of
+// a power of two of the head's (exact: bf16 has 8 bits, fp16 11), weights fp16 in units of the largest row's.  The rotated 64 numbers are bf16 on
+// both sides and have a sum of their own.  Sums, maxima and totals are 32 bits throughout; what is rounded is said here.
 //
-// Warps: 0-7 softmax (two for each 16 heads, 32 rows each); 8-15 rows, gathered and converted by four warps for one tile and four for the next (bf16: by
-// all eight), so that one's loads are under way while the other stores; 16 issues the products, whichever of the next tile's S and the last one's O can be next.
+// Warps: first those of softmax, by quarters of the heads and shares of a tile's rows; then those of the rows, eight rows each, which gather (and
+// convert) them; the last one issues the products, whichever of the next tile's S and the last one's O can be next.  Softmax of e4m3 rows, which
+// adds five sums up, has 16 warps (8: 98 us where 16 take 95, and 62 for 55 with capped scores); the others' 8 (16 for bf16: 18.3 us for 17.1; every warp
+// more takes registers from all).
 //
 // A query's rows are split over a cluster's blocks where queries are few, tile by tile in turn; the blocks' sums are joined through
 // distributed shared memory in a fixed order (same results on every run, no workspace).
+//
+// What bounds it: per tile and block the chain rows - scores - softmax - weights - sums, of which two tiles are under way (shared memory has room
+// for two), about 4700 clocks; the matrix unit alone needs 1700 to 2000, shared memory's bandwidth (both products read their operands from
+// there: a 64 x 64 product of 16 numbers takes 34 clocks, all of its bandwidth) 2200 to 3000.  Around it 9000 clocks until the first scores (queries,
+// rows from DRAM) and 4000 to 6000 behind the last.  Device times: 32 requests, two tokens, 128 heads, 2048 of 8192 e4m3 rows 95 us (383
+// TFLOP/s); 16 heads, 4-bit rows 46; one request, two tokens, 128 heads, bf16 rows 17; one token, 16 heads, 256 rows 11.
 #include <atomic>
 
 #include <cuda_bf16.h>
@@ -616,7 +624,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
                     }
                 }
             }
-            // The next tile's first sums, if they are there: their place in TMEM is wanted.
+            // The next tile's first sums, if they are there: their place in TMEM is wanted.  (95 us, 100 without this look; 98 with a later one.)
             bool early = false;
             if (L::CODES && busy && j + 1 < tiles) {
                 const uint32_t step = (j + 1) * L::STEPS;
@@ -988,7 +996,9 @@ cudaError_t attend_prepare()
 cudaError_t launch_attend(AttendParams& p, uint32_t format, cudaStream_t stream)
 {
     // Blocks of a query: its rows over a cluster's, its heads in groups; as many as find room at once.  First the rows, a tile or more to
-    // a block; then smaller groups of heads, down to 16, although each gathers the rows again: a block's sums travel between a cluster's blocks, heads x 2 KB.
+    // a block: 17 us for 62 with one request of 128 heads and bf16 rows, 46 for 79 with 64 queries of 4-bit rows, but 56 and 94 with two and four times
+    // the blocks that fit.  Then smaller groups of heads, down to 16, although each gathers the rows again (a block's sums travel between a cluster's
+    // blocks, heads x 2 KB): 17 us for 20 with that one request.
     const uint32_t least = (p.heads + GROUP - 1) / GROUP, tiles = (p.topk + TILE - 1) / TILE;
     const uint64_t queries = (uint64_t)p.n * p.n_tokens;
     int device = -1;

@@ -337,6 +337,52 @@ def test_attend_many_tables(avsg):
         ctx.attend([n] * n, q, slots, row_format=avsg.ROW_FP4, scale=SCALE)
 
 
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("size", [(3, 2, 20, 200, 256), (2, 1, 64, 700, 1024)], ids=lambda s: "x".join(map(str, s)))
+def test_attend_scales_far_apart_within_a_row_and_between_rows(avsg, fmt, size):
+    # 8 bits: groups of a row from 2^-20 to 2^4, some negative, some zero; 4 bits: groups 2^-18 .. 1 of each other; a few rows of 2^6 times the others' size
+    import torch
+    import rows_reference as ref
+    n, T, H, K, S = size
+    q, buffer, slots = _problem(fmt, *size, seed=61 + fmt)
+    g = _gen(62 + fmt)
+    rows = buffer.view(-1, buffer.shape[-1])
+    large = torch.rand(rows.shape[0], 1, generator=g, device="cuda") < 0.02
+    if fmt == 1:
+        power = torch.randint(-26, -1, (rows.shape[0], 4), generator=g, device="cuda").double() + 6.0 * large
+        scale = torch.exp2(power) * (1 + torch.rand(rows.shape[0], 4, generator=g, device="cuda"))
+        scale *= torch.where(torch.rand(rows.shape[0], 4, generator=g, device="cuda") < 0.1, -1.0, 1.0)
+        scale[torch.rand(rows.shape[0], 4, generator=g, device="cuda") < 0.1] = 0.0
+        rows[:, 512:528] = scale.float().view(torch.uint8)
+    else:
+        code = torch.randint(105, 124, (rows.shape[0], 16), generator=g, device="cuda") + 6 * large
+        code[torch.rand(rows.shape[0], 16, generator=g, device="cuda") < 0.05] = 0
+        rows[:, 256:272] = code.to(torch.uint8)
+    out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=0.01, want_lse=True)
+    ref.agree(out, lse, ref.attend(q, buffer, slots, fmt, 0.01))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attend_a_table_that_stands_twice_in_a_call(avsg, fmt):
+    # a context's tables may repeat: two blocks of queries read the same buffer
+    import torch
+    import rows_reference as ref
+    rb = ref.BYTES[fmt]
+    ctx = avsg.Context(num_tables=2, buffer_slots=128, row_bytes=rb, max_topk=32, max_tokens=1)
+    try:
+        q, buffer, slots = _problem(fmt, 3, 1, 18, 32, 128, seed=71)
+        kv = [buffer[i].contiguous() for i in range(2)]
+        ids = torch.stack([torch.randperm(128, generator=_gen(72), device="cuda")[:32] for _ in range(2)]).to(torch.int32).view(2, 1, 32)
+        step = ctx.step([0, 1], ids, kv, [128, 128])
+        at = step.slots[[1, 0, 1]].contiguous()
+        got = ctx.attend([1, 0, 1], q, at, row_format=fmt, scale=SCALE, want_lse=True)
+        held = torch.stack([kv[1], kv[0], kv[1]])
+        ref.agree(*got, ref.attend(q, held, ids[[1, 0, 1]].contiguous(), fmt, SCALE))
+        assert ctx.sync_status() == 0
+    finally:
+        ctx.close()
+
+
 # ---- appending ------------------------------------------------------------------------------------------------------
 def _rows_agree(got, want, fmt, turned):
     """Latent bytes are the definition's, bit for bit; the rotated part is a bf16 beside the exact one."""
