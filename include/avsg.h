@@ -505,7 +505,8 @@ typedef struct {
  *
  * ctx may be NULL.  With a context, table_ids names its tables, problems go to the context's status word, and
  * row_format has to be of the context's row_bytes.  Without one table_ids is
- * NULL, the call runs on the device that `positions` lies on, and problems go to *status.
+ * NULL, the call runs on the device that `positions` lies on, and problems go to *status; the first call on a device loads its kernels and
+ * belongs outside any stream capture.  All device memory of a call lies on one device (with a context: its device).
  * Asynchronous on cuda_stream; host arrays are consumed before the call returns.  Two tokens of one call must not name the
  * same row: its bytes would be some of one and some of the other.
  */
@@ -563,7 +564,8 @@ int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
  *
  * ctx may be NULL.  With a context, rows are read from its buffers (buffer NULL), table_ids names the tables, which may repeat, and
  * row_format has to be of the context's row_bytes.  Without one table_ids is NULL and buffer holds n tables of buffer_slots rows
- * (avsg_step_noalloc's layout); the call runs on the device that `slots` lies on.  Asynchronous on cuda_stream, nothing is allocated
+ * (avsg_step_noalloc's layout); the call runs on the device that `slots` lies on, and the first one on a device belongs outside any stream
+ * capture.  All device memory of a call lies on one device (with a context: its device).  Asynchronous on cuda_stream, nothing is allocated
  * and no state is kept: calls may overlap one another.
  */
 typedef struct {
@@ -579,7 +581,7 @@ typedef struct {
     const void     *q;              /* DEVICE bf16 [n][n_tokens][heads][576]                                */
     uint64_t        q_stride[3];    /* bytes between tables, tokens, heads; multiples of 16                 */
     void           *out;            /* DEVICE out bf16 [n][n_tokens][heads][512]                            */
-    uint64_t        out_stride[3];  /* bytes between tables, tokens, heads; multiples of 16                 */
+    uint64_t        out_stride[3];  /* likewise, 0 only between one                                         */
     float          *lse;            /* DEVICE out [n][n_tokens][heads], natural logarithm, or NULL          */
     float           scale;          /* finite                                                               */
     float           softcap;        /* > 0, or 0: none                                                      */

@@ -657,6 +657,12 @@ def _stream_number(stream):
     return stream if stream is None or type(stream) is int else _stream_handle(stream) or 0
 
 
+def _rows_in(kv, bytes_: int, stride) -> int:
+    """Rows that a cache given as a tensor has room for."""
+    span = (sum((size - 1) * step for size, step in zip(kv.shape, kv.stride())) + 1) * kv.element_size() if kv.numel() else 0
+    return 0 if span < bytes_ else min((span - bytes_) // (stride or bytes_) + 1, 0x80000000)
+
+
 def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[Rope] = None, rows=None, row_stride=None, kv_rows=None,
            want_values: bool = False, values=None, status=None, stream=None, _ctx=None, _tables=None):
     """avsg_append: the rows of new positions, rotated and quantised on their way into the cache.
@@ -664,7 +670,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     latent [n, n_tokens, 512] and rope_part [n, n_tokens, 64]: CUDA tensors of one type (bf16, fp16, fp32), parts of a wider
     projection too; positions int32 [n, n_tokens], negative = padding; rows int32 like positions: where a token's row goes, if
     not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
-    table, as avsg_step takes them; a tensor [rows, bytes] is a pool that all tables share.  Returns the values tensor (bf16 [n,
+    table, as avsg_step takes them (without kv_rows a tensor's own bytes are the limit, an address has none); a tensor [rows, bytes] is a pool that all tables share.  Returns the values tensor (bf16 [n,
     n_tokens, 576], what the rows stand for) where one is wanted, else None."""
     import torch
     if _append_fn is None:
@@ -708,6 +714,9 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
         _need(len(kv) == n, "append: one cache per table")
         owner, kv_base = _c_array("Q", [_addr(k) for k in kv], n)
         keep.append(owner)
+        if kv_rows is None and all(hasattr(k, "stride") and hasattr(k, "element_size") for k in kv):
+            # a tensor's own bytes are the cache's limit
+            kv_rows = [_rows_in(k, row_bytes(row_format), None if row_stride is None else row_stride[i]) for i, k in enumerate(kv)]
     strides, strides_at = _c_array("Q", row_stride, n)
     limits, limits_at = _c_array("I", kv_rows, n)
     tables, tables_at = _c_array("I", _tables, n)

@@ -156,6 +156,14 @@ int distinct_tables(avsg_ctx* c, const uint32_t* table_ids, uint32_t n)
     return AVSG_OK;
 }
 
+// An array of a call of rows has to lie on the context's device.
+int on_device(avsg_ctx* c, const void* p)
+{
+    int device = -1;
+    const int rc = device_of(p, &device);
+    return rc != AVSG_OK ? rc : device == c->cfg.device ? AVSG_OK : AVSG_EINVAL;
+}
+
 int check_args(avsg_ctx* c, const avsg_step_args* a)
 {
     if (!c || !a) return AVSG_EINVAL;
@@ -730,6 +738,7 @@ int avsg_append(avsg_ctx* c, const avsg_append_args* a, void* cuda_stream)
     if (rc != AVSG_OK) return rc;
     if (!a->table_ids || a->status || a->n > c->cfg.num_tables || row_bytes_of(a->row_format) != c->cfg.row_bytes) return AVSG_EINVAL;
     if ((rc = distinct_tables(c, a->table_ids, a->n)) != AVSG_OK) return rc;
+    if ((rc = on_device(c, a->positions)) != AVSG_OK) return rc;
     DeviceGuard guard(c->cfg.device);
     if (!guard.ok) return AVSG_ECUDA;
     return append_run(a, c->d_status, stream);
@@ -739,11 +748,12 @@ int avsg_attend(avsg_ctx* c, const avsg_attend_args* a, void* cuda_stream)
 {
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (!c) return attend_bare(a, stream);
-    const int rc = check_attend(a);
+    int rc = check_attend(a);
     if (rc != AVSG_OK) return rc;
     if (!a->table_ids || a->buffer || a->buffer_slots || a->buffer_row_bytes || a->status || row_bytes_of(a->row_format) != c->cfg.row_bytes)
         return AVSG_EINVAL;
     for (uint32_t i = 0; i < a->n; ++i) if (a->table_ids[i] >= c->cfg.num_tables) return AVSG_EINVAL;
+    if ((rc = on_device(c, a->slots)) != AVSG_OK) return rc;
     DeviceGuard guard(c->cfg.device);
     if (!guard.ok) return AVSG_ECUDA;
     return attend_run(a, c->d_buffer, c->cfg.buffer_slots, c->cfg.row_bytes, c->d_status, stream);

@@ -9,6 +9,20 @@ namespace avsg {
 
 namespace {
 
+constexpr int MAX_DEVICES = 64;
+std::mutex g_mutex;
+bool g_ready[MAX_DEVICES] = {false};
+
+bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uint64_t>(p) & (to - 1)) == 0; }
+
+bool good_rope(const avsg_rope* r)
+{
+    for (double f : r->inv_freq) if (!isfinite(f)) return false;
+    return isfinite(r->scale) && r->halves <= 1;
+}
+
+}  // namespace
+
 // What a call without a context runs on: the device that one of its arrays lies on.
 int device_of(const void* p, int* device)
 {
@@ -19,9 +33,7 @@ int device_of(const void* p, int* device)
     return AVSG_OK;
 }
 
-constexpr int MAX_DEVICES = 64;
-std::mutex g_mutex;
-bool g_ready[MAX_DEVICES] = {false};
+namespace {
 
 // Makes `device` current; its kernels are loaded by the first call on it.
 struct OnDevice {
@@ -40,14 +52,6 @@ struct OnDevice {
     }
     ~OnDevice() { if (other) cudaSetDevice(prev); }
 };
-
-bool aligned(const void* p, uint64_t to) { return (reinterpret_cast<uint64_t>(p) & (to - 1)) == 0; }
-
-bool good_rope(const avsg_rope* r)
-{
-    for (double f : r->inv_freq) if (!isfinite(f)) return false;
-    return isfinite(r->scale) && r->halves <= 1;
-}
 
 }  // namespace
 
@@ -83,10 +87,12 @@ int append_run(const avsg_append_args* a, uint32_t* status, cudaStream_t stream)
 {
     // Every address that the GPU cannot reach is refused before anything is launched.
     uint64_t base[ROWS_MAX_TABLES];
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return AVSG_ECUDA; }
     for (uint32_t i = 0; i < (a->kv_base ? a->n : 1u); ++i) {
         cudaPointerAttributes at;
         if (cudaPointerGetAttributes(&at, a->kv_base ? a->kv_base[i] : a->kv) != cudaSuccess) { cudaGetLastError(); return AVSG_EINVAL; }
-        if (at.type == cudaMemoryTypeUnregistered || !at.devicePointer) return AVSG_EINVAL;
+        if (at.type == cudaMemoryTypeUnregistered || !at.devicePointer || (at.type == cudaMemoryTypeDevice && at.device != device)) return AVSG_EINVAL;
         base[i] = reinterpret_cast<uint64_t>(at.devicePointer);
     }
     AppendParams p;
@@ -120,6 +126,8 @@ int check_attend(const avsg_attend_args* a)
     if (a->heads > 1024 || (uint64_t)a->n * a->n_tokens > (1u << 24) || a->topk > (1u << 24)) return AVSG_EUNSUPPORTED;
     if (!a->slots || !a->q || !a->out || !aligned(a->slots, 4) || !aligned(a->q, 16) || !aligned(a->out, 16)) return AVSG_EINVAL;
     for (int i = 0; i < 3; ++i) if (a->q_stride[i] % 16 || a->out_stride[i] % 16) return AVSG_EINVAL;
+    // (queries may be broadcast; outputs may not)
+    if ((a->n > 1 && a->out_stride[0] == 0) || (a->n_tokens > 1 && a->out_stride[1] == 0) || (a->heads > 1 && a->out_stride[2] == 0)) return AVSG_EINVAL;
     if (!aligned(a->lse, 4) || !aligned(a->ids, 4) || !aligned(a->positions, 4) || !aligned(a->spans, 4) || !aligned(a->slopes, 4) || !aligned(a->status, 4))
         return AVSG_EINVAL;
     if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.f) return AVSG_EINVAL;

@@ -59,6 +59,8 @@ cudaError_t attend_prepare();
 cudaError_t launch_attend(AttendParams& p, uint32_t format, cudaStream_t stream);
 
 // The parts of the two calls: the checks, and what follows them with a context's buffers and status word or the caller's own.
+// The device that an array lies on (AVSG_EINVAL: on none).
+int device_of(const void* p, int* device);
 int check_append(const avsg_append_args* a);
 int check_attend(const avsg_attend_args* a);
 int append_run(const avsg_append_args* a, uint32_t* status, cudaStream_t stream);

@@ -194,3 +194,69 @@ def test_calls_of_a_context_both_ways(avsg, binding):                         # 
         finally:
             ctx.close()
     assert _same(*got)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_to_a_list_of_tensors_stays_within_them(avsg, binding, fmt):   # noqa: F811
+    import torch
+    b, module = binding
+    n, T, R = 2, 4, 6
+    bytes_ = avsg.row_bytes(fmt)
+    g = _gen(8)
+    latent = torch.randn(n, T, 512, generator=g, device="cuda").to(torch.bfloat16)
+    part = torch.randn(n, T, 64, generator=g, device="cuda").to(torch.bfloat16)
+    positions = torch.tensor([[0, 5, 6, 7], [1, 2, 3, 9]], dtype=torch.int32, device="cuda")
+    for way in (module, False):
+        b._tensor_calls = way
+        pool = torch.zeros(n, 12, bytes_, dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        avsg.append(latent, part, positions, [pool[0, :R], pool[1, :R]], row_format=fmt, status=status)
+        assert int(status) == avsg.STATUS_BAD_ID
+        written = (pool != 0).any(2).cpu()
+        assert written[0].nonzero().flatten().tolist() == [0, 5] and written[1].nonzero().flatten().tolist() == [1, 2, 3]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_what_lies_elsewhere_or_shares_its_place_is_refused(avsg, binding, fmt):                   # noqa: F811
+    import ctypes
+    import torch
+    b, module = binding
+    q, buffer, slots = _problem(fmt, 2, 2, 8, 32, 64, seed=9)
+    shared = torch.empty(1, 1, 1, 512, dtype=torch.bfloat16, device="cuda").expand(2, 2, 8, 512)
+    for x in _both(binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, out=shared)):
+        assert isinstance(x, avsg.AvsgError) and x.code == avsg.EINVAL
+    # slots and positions in host memory, through the C entry with a context
+    ctx = avsg.Context(num_tables=2, buffer_slots=64, row_bytes=avsg.row_bytes(fmt), max_topk=32, max_tokens=2)
+    try:
+        host = torch.zeros(2 * 2 * 32, dtype=torch.int32).pin_memory()
+        out = torch.empty(2, 2, 8, 512, dtype=torch.bfloat16, device="cuda")
+        ids = (ctypes.c_uint32 * 2)(0, 1)
+        a = avsg.AvsgAttendArgs()
+        a.n, a.n_tokens, a.topk, a.heads, a.row_format, a.scale = 2, 2, 32, 8, fmt, 1.0
+        a.table_ids, a.slots, a.q, a.out = ctypes.addressof(ids), host.data_ptr(), q.data_ptr(), out.data_ptr()
+        for k, (s, t) in enumerate(zip(q.stride(), out.stride())):
+            if k < 3:
+                a.q_stride[k], a.out_stride[k] = 2 * s, 2 * t
+        assert avsg.load_library().avsg_attend(ctx._h, ctypes.byref(a), None) == avsg.EINVAL
+        latent = torch.zeros(2, 2, 576, dtype=torch.bfloat16, device="cuda")
+        kv = torch.zeros(2, 64, avsg.row_bytes(fmt), dtype=torch.uint8, device="cuda")
+        p = avsg.AvsgAppendArgs()
+        p.n, p.n_tokens, p.row_format, p.type = 2, 2, fmt, 0
+        p.table_ids, p.latent, p.rope_part, p.positions, p.kv = ctypes.addressof(ids), latent.data_ptr(), latent.data_ptr() + 1024, host.data_ptr(), kv.data_ptr()
+        for k in range(2):
+            p.latent_stride[k] = p.rope_stride[k] = (2304, 1152)[k]
+        p.kv_table_stride = 64 * avsg.row_bytes(fmt)
+        assert avsg.load_library().avsg_append(ctx._h, ctypes.byref(p), None) == avsg.EINVAL
+        torch.cuda.synchronize()
+        assert ctx.sync_status() == 0
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_queries_may_be_broadcast(avsg, binding, fmt):                        # noqa: F811
+    import torch
+    q, buffer, slots = _problem(fmt, 3, 2, 8, 40, 64, seed=10)
+    one = q[:1, :1].expand(3, 2, 8, 576)
+    for got in _both(binding, lambda: avsg.attend(one, buffer, slots, row_format=fmt, scale=SCALE)):
+        assert torch.equal(got, avsg.attend(one.contiguous(), buffer, slots, row_format=fmt, scale=SCALE))

@@ -109,3 +109,29 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu():
     with pytest.raises(avsg.AvsgError):
         avsg.append(torch.zeros(1, 1, 512), torch.zeros(1, 1, 64), torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, 4, 656, dtype=torch.uint8),
                     row_format=avsg.ROW_FP8)
+
+
+@pytest.mark.parametrize("i,size", [(0, dict(n=2)), (1, dict(n_tokens=2)), (2, dict(heads=2))])
+def test_attend_refuses_outputs_that_share_their_place(i, size):
+    strides = [4096, 2048, 1024]
+    strides[i] = 0
+    a = avsg.AvsgAttendArgs()
+    a.n = a.n_tokens = a.topk = a.heads = 1
+    a.row_format, a.buffer_slots, a.scale = avsg.ROW_FP8, 32, 1.0
+    a.slots = a.q = a.out = a.buffer = P
+    for k, v in size.items():
+        setattr(a, k, v)
+    for k in range(3):
+        a.out_stride[k] = strides[k]
+    assert avsg.load_library().avsg_attend(None, ctypes.byref(a), None) == avsg.EINVAL
+
+
+def test_rows_in_a_cache_given_as_a_tensor():
+    import torch
+    from paper_2609_37538_b200.binding import _rows_in
+    flat = torch.zeros(10 * 656 + 100, dtype=torch.uint8)
+    assert _rows_in(flat, 656, None) == 10 and _rows_in(flat[:655], 656, None) == 0 and _rows_in(flat[:0], 656, None) == 0
+    assert _rows_in(flat[:6560].view(10, 656), 656, None) == 10
+    wide = torch.zeros(7, 672, dtype=torch.uint8)
+    assert _rows_in(wide[:, :656], 656, 672) == 7 and _rows_in(wide[:, :640], 656, 672) == 6
+    assert _rows_in(torch.zeros(4, 164, dtype=torch.float32), 656, None) == 4
