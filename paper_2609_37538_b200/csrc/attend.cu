@@ -25,7 +25,7 @@
 // What bounds it: per tile and block the chain rows - scores - softmax - weights - sums, of which two tiles are under way (shared memory has room
 // for two), about 4700 clocks; the matrix unit alone needs 1700 to 2000, shared memory's bandwidth (both products read their operands from
 // there: a 64 x 64 product of 16 numbers takes 34 clocks, all of its bandwidth) 2200 to 3000.  Around it 9000 clocks until the first scores (queries,
-// rows from DRAM) and 4000 to 6000 behind the last.  Device times: 32 requests, two tokens, 128 heads, 2048 of 8192 e4m3 rows 95 us (383
+// rows from DRAM) and 4000 to 6000 behind the last.  Device times: 32 requests, two tokens, 128 heads, 2048 of 8192 e4m3 rows 94 us (387
 // TFLOP/s); 16 heads, 4-bit rows 46; one request, two tokens, 128 heads, bf16 rows 17; one token, 16 heads, 256 rows 11.
 #include <atomic>
 
@@ -624,13 +624,8 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
                     }
                 }
             }
-            // The next tile's first sums, if they are there: their place in TMEM is wanted.  (95 us, 100 without this look; 98 with a later one.)
-            bool early = false;
-            if (L::CODES && busy && j + 1 < tiles) {
-                const uint32_t step = (j + 1) * L::STEPS;
-                early = __all_sync(0xffffffffu, barrier_done(bars + SUM_FULL + 8 * (step % SLOTS), step / SLOTS & 1u));
-                if (early) take(j + 1, 0);
-            }
+            // The next tile's first sums, already: their place in TMEM is wanted.  (94 us; 100 where they are taken after the weights are out.)
+            if (L::CODES) take(j + 1, 0);
             if (busy) {
                 const float inverse = 1.f / unit;
                 const uint32_t piece = base + (L::CODES ? L::AT_WEIGHTS : L::AT_TILES + b * L::TILE_BYTES + L::ROPE_PIECE * PIECE);
@@ -653,7 +648,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
             tmem_before_sync();
             arrive(bars + WEIGHTS + 8 * b, lane);
             ask_ids(j + 1);
-            if (!early) take(j + 1, 0);
+            if (!L::CODES) take(j + 1, 0);
 #pragma unroll
             for (uint32_t g = 1; g < L::STEPS; ++g) take(j + 1, g);
         }
