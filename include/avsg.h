@@ -584,7 +584,7 @@ typedef struct {
     uint64_t        out_stride[3];  /* likewise, 0 only between one                                         */
     float          *lse;            /* DEVICE out [n][n_tokens][heads], natural logarithm, or NULL          */
     float           scale;          /* finite                                                               */
-    float           softcap;        /* > 0, or 0: none                                                      */
+    float           softcap;        /* > 0 (2^-126 or more), or 0: none                                     */
     const int32_t  *ids;            /* DEVICE [n][n_tokens][topk]: the positions that the slots hold (indices of
                                        avsg_step); NULL unless spans or slopes are given                    */
     const int32_t  *positions;      /* DEVICE [n][n_tokens]: the queries' positions; NULL unless slopes or rope are given */

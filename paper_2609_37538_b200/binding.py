@@ -643,11 +643,13 @@ _tensor_calls = False                                # the extension module that
 def _rows_functions():
     global _append_fn, _attend_fn, _tensor_calls
     lib = load_library()
+    import torch
     try:
         from . import _tensor_calls as module
-    except ImportError:                              # not built, or for another torch: the same calls are marshalled below
-        pass
-    else:
+    except ImportError:                              # not built: the same calls are marshalled below
+        module = None
+    _tensor_calls = False
+    if module and module.built_for == torch.__version__:
         module.set_library(_address_of(lib.avsg_append), _address_of(lib.avsg_attend), _address_of(lib.avsg_row_bytes))
         _tensor_calls = module
     _append_fn, _attend_fn = _ROWS_CALL(_address_of(lib.avsg_append)), _ROWS_CALL(_address_of(lib.avsg_attend))

@@ -52,7 +52,7 @@ def build_tensor_calls(force: bool = False):
         headers = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), "/usr/local/cuda/include"]
         tmp = TENSOR_CALLS + ".tmp.%d" % os.getpid()
         subprocess.check_call([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden",
-                               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                               "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, '-DBUILT_FOR="%s"' % torch.__version__,
                                "-I", sysconfig.get_paths()["include"], "-I", INCLUDE] + [x for h in headers for x in ("-isystem", h)] +
                               ["-o", tmp, TENSOR_CALLS_SOURCE, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
                                "-ltorch_python"])

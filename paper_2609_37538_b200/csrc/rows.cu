@@ -1,4 +1,5 @@
 // avsg_append and avsg_attend: argument checks and the two calls without a context (with one: avsg_api.cu).
+#include <float.h>
 #include <math.h>
 #include <mutex>
 #include <string.h>
@@ -130,7 +131,7 @@ int check_attend(const avsg_attend_args* a)
     if ((a->n > 1 && a->out_stride[0] == 0) || (a->n_tokens > 1 && a->out_stride[1] == 0) || (a->heads > 1 && a->out_stride[2] == 0)) return AVSG_EINVAL;
     if (!aligned(a->lse, 4) || !aligned(a->ids, 4) || !aligned(a->positions, 4) || !aligned(a->spans, 4) || !aligned(a->slopes, 4) || !aligned(a->status, 4))
         return AVSG_EINVAL;
-    if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.f) return AVSG_EINVAL;
+    if (!isfinite(a->scale) || !isfinite(a->softcap) || a->softcap < 0.f || (a->softcap > 0.f && a->softcap < FLT_MIN)) return AVSG_EINVAL;
     if ((a->spans || a->slopes) && !a->ids) return AVSG_EINVAL;
     if ((a->slopes || a->rope) && !a->positions) return AVSG_EINVAL;
     if (a->rope && !good_rope(a->rope)) return AVSG_EINVAL;

@@ -286,5 +286,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensor_calls", nullptr, -1, metho
 
 PyMODINIT_FUNC PyInit__tensor_calls()
 {
-    return PyModule_Create(&module);
+    PyObject* m = PyModule_Create(&module);
+    if (!m || PyModule_AddStringConstant(m, "built_for", BUILT_FOR) < 0) return nullptr;          // (this version of torch)
+    return m;
 }

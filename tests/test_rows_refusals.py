@@ -135,3 +135,22 @@ def test_rows_in_a_cache_given_as_a_tensor():
     wide = torch.zeros(7, 672, dtype=torch.uint8)
     assert _rows_in(wide[:, :656], 656, 672) == 7 and _rows_in(wide[:, :640], 656, 672) == 6
     assert _rows_in(torch.zeros(4, 164, dtype=torch.float32), 656, None) == 4
+
+
+def test_attend_refuses_a_cap_that_counts_as_zero():
+    assert _attend(softcap=1e-40) == avsg.EINVAL
+
+
+def test_the_extension_module_serves_the_torch_that_it_was_built_for(monkeypatch):
+    import torch
+    from paper_2609_37538_b200 import binding as b
+    b._rows_functions()
+    module = b._tensor_calls
+    try:
+        if module:
+            assert module.built_for == torch.__version__
+        monkeypatch.setattr(torch, "__version__", "0.0.1")
+        b._rows_functions()
+        assert b._tensor_calls is False and b._attend_fn is not None
+    finally:
+        b._tensor_calls = module
