@@ -164,7 +164,7 @@ __device__ __forceinline__ void put_codes(uint4 body, int c, int unit, uint32_t 
         const int power = (int)e - unit;                                        // scale / unit is 2^power, power <= 13
         if (power >= -13 && e != 255u) {
             // The upper bytes of 0, .5, 1, 1.5 and 2, 3, 4, 6 times 2^power as fp16 (the lower are zero), looked up by a code's last three bits, four
-            // codes at a time; signs beside.  (A conversion and a product for two codes: a fifth more instructions.)
+            // codes at a time; signs beside.  (By a conversion and a product for two codes: 46.4 us for 46.0.)
             const uint32_t small = 0x3E3C3800u + (uint32_t)(4 * power) * 0x01010100u, large = 0x46444240u + (uint32_t)(4 * power) * 0x01010101u;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
