@@ -52,8 +52,7 @@ struct Layout {
     static constexpr bool HALF = FORMAT != AVSG_ROW_BF16;                       // fp16 weights and values
     static constexpr bool CODES = FORMAT == AVSG_ROW_FP8;                       // scores from e4m3 codes
     static constexpr uint32_t SOFTMAX_WARPS = CODES ? 16 : 8, SHARES = SOFTMAX_WARPS / 4, EACH = TILE / SHARES;        // rows of a tile to each
-    static constexpr uint32_t TURNS = 1;           // groups of eight row warps that take tiles in turn
-    static constexpr uint32_t ROW_WARPS = 8 * TURNS, WARPS = SOFTMAX_WARPS + ROW_WARPS + 1, THREADS = 32 * WARPS;
+    static constexpr uint32_t ROW_WARPS = 8, WARPS = SOFTMAX_WARPS + ROW_WARPS + 1, THREADS = 32 * WARPS;
     static constexpr uint32_t STEPS = CODES ? 3 : 1;                            // of a tile's S: two latent sums, two, the rotated one; or all at once
     static constexpr uint32_t PARTS = CODES ? 3 : 2;                            // in which its products are issued
     static constexpr uint32_t ROPE_PIECE = CODES ? BODY / 2 : BODY;             // of a tile: the rotated numbers (behind 128 or 64 numbers a line)
@@ -284,10 +283,9 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
             }
         }
     }
-    // A row warp's first rows too: a lane has every fourth 16-byte unit of one of its warp's eight lines.
+    // A row warp's first slots too: lane l speaks for line l % 8 of its warp's eight.
     const uint32_t sub = lane / 8u, group_warp = (warp - SOFTMAX_WARPS) & 7u, line = group_warp * 8u + lane % 8u;
     const uint8_t* rows = p.buffer + (uint64_t)(p.mapped ? p.table_id[table] : table) * p.table_stride;
-    const uint32_t first_tile = L::TURNS > 1 ? (warp - SOFTMAX_WARPS) / 8u : 0u;
     int32_t begin = INT32_MIN, end = INT32_MAX;
     struct Place { int32_t slot, id; };
     auto place = [&](uint32_t j) -> Place {                 // the slot (and id) of tile j's line
@@ -307,8 +305,8 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
     Place here = {-1, 0}, next = {-1, 0};                   // of the next tile whose rows are asked for, and the one behind
     if (warp >= SOFTMAX_WARPS && warp < SOFTMAX_WARPS + ROW_WARPS) {
         if (p.spans) { begin = p.spans[2 * item]; end = p.spans[2 * item + 1]; }
-        here = place(first_tile);
-        next = place(first_tile + L::TURNS);
+        here = place(0);
+        next = place(1);
     }
     if (warp == WARPS - 1) {
         if (lane == 0) {
@@ -690,24 +688,24 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
             auto advance = [&](uint32_t j) {                // tile j's rows, whose places are known by now
                 row = row_of(here);
                 here = next;
-                next = j + 2 * L::TURNS < tiles ? place(j + 2 * L::TURNS) : Place{-1, 0};
+                next = j + 2 < tiles ? place(j + 2) : Place{-1, 0};
                 for (int i = 0; i < 2; ++i) from[i] = row_at(row, 4u * i + lane / 8u);
                 part.scales = unit_at(lane < 8u ? row : nullptr, 16);
             };
             auto ask = [&](int c, int i) { part.body[c][i] = unit_at(from[i], 8u * c + lane % 8u); };
             auto ask_rope = [&](int i) { part.rope[i] = unit_at(from[i], 17u + lane % 8u); };
-            if (first_tile < tiles) {
-                advance(first_tile);
+            if (tiles) {
+                advance(0);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) { ask(c, 0); ask(c, 1); }
                 ask_rope(0); ask_rope(1);
             }
-            for (uint32_t j = first_tile; j < tiles; j += L::TURNS) {
+            for (uint32_t j = 0; j < tiles; ++j) {
                 const uint32_t b = j & 1u, tile = base + L::AT_TILES + b * L::TILE_BYTES;
                 const uint4 scales = part.scales;
                 const uint32_t unit = nibble_unit(scales), seen = __ballot_sync(0xffffffffu, row != nullptr);
                 const uint32_t top = __reduce_max_sync(0xffffffffu, lane < 8u && row ? unit : 0u);
-                advance(j + L::TURNS);                      // (beyond the last tile: nothing)
+                advance(j + 1);                             // (beyond the last tile: nothing)
                 if (j >= 2 && !passed(FREE, j - 2)) break;
                 if (lane == 0) {
                     shared[L::AT_SEEN + 8 * b + group_warp] = (uint8_t)seen;
