@@ -768,12 +768,13 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     if _ctx is None:
         held = buffer.shape
         if buffer.get_device() != device or buffer.dtype is not torch.uint8 or len(held) != 3 or held[0] != n or held[2] != row_bytes(row_format) or \
-                buffer.stride(2) != 1 or (n > 1 and buffer.stride(0) != buffer.stride(1) * held[1]):
+                buffer.stride(2) != 1 or (n > 1 and held[1] > 1 and buffer.stride(0) != buffer.stride(1) * held[1]):
             raise AvsgError(EINVAL, "attend: buffer is a uint8 tensor [n, slots, row bytes] on q's device, its tables one behind another")
         # (an expanded row has a stride of 0, which the library would take for the bytes of a row)
         if (held[1] > 1 and buffer.stride(1) < held[2]) or (n > 1 and buffer.stride(0) < held[2]):
             raise AvsgError(EINVAL, "attend: rows of buffer share their place")
-        rows_at, rows, row_step = buffer.data_ptr(), held[1], (buffer.stride(1) if held[1] > 1 else 0)
+        # (tables of one row are as far apart as their rows; the stride between rows says nothing then)
+        rows_at, rows, row_step = buffer.data_ptr(), held[1], (buffer.stride(1) if held[1] > 1 else buffer.stride(0) if n > 1 else 0)
     else:
         _need(len(_tables) == n, "attend: one table per block of queries")
         owner, tables_at = _c_array("I", _tables, n)

@@ -139,12 +139,13 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     } else {
         const at::Tensor* b = strided(a[3], at::kByte, 3);
         if (ctx || a[1] != Py_None || !b || b->get_device() != device || b->size(0) != n || !fits(b->size(1)) ||
-            b->size(2) != row_bytes(s.row_format) || (n > 1 && b->stride(0) != b->stride(1) * b->size(1)) ||
+            b->size(2) != row_bytes(s.row_format) || (n > 1 && b->size(1) > 1 && b->stride(0) != b->stride(1) * b->size(1)) ||
             (b->size(1) > 1 && b->stride(1) < b->size(2)) || (n > 1 && b->stride(0) < b->size(2)))
             return not_handled();
         s.buffer = b->data_ptr();
         s.buffer_slots = b->size(1);
-        s.buffer_row_bytes = b->size(1) > 1 ? b->stride(1) : 0;
+        // (tables of one row are as far apart as their rows; the stride between rows says nothing then)
+        s.buffer_row_bytes = b->size(1) > 1 ? b->stride(1) : n > 1 ? b->stride(0) : 0;
     }
     if (!packed(a[4], at::kInt, {n, T, K}, device, &at) || !at) return not_handled();
     s.slots = reinterpret_cast<const int32_t*>(at);

@@ -35,3 +35,21 @@ def test_a_buffer_whose_rows_share_their_place_is_refused(avsg, binding, fmt):  
                  buffer.as_strided((2, 32, size), (32 * 16, 16, 1)), buffer.as_strided((2, 1, size), (0, 0, 1))):
         _refused(avsg, binding, lambda: avsg.attend(q, held, slots * 0, row_format=fmt, scale=SCALE))
     _refused(avsg, binding, lambda: avsg.attend(q[:1], buffer[:1, :1].expand(1, 32, size), slots[:1], row_format=fmt, scale=SCALE))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_tables_of_one_row_with_room_behind_them(avsg, binding, fmt):             # noqa: F811
+    # one slot per table: the tables are apart by the first stride, whatever the second (of a single row) says
+    import torch
+    import rows_reference as ref
+    n, T, H = 3, 2, 8
+    q, buffer, slots = _problem(fmt, n, T, H, 1, 1, seed=80)
+    want = ref.attend(q, buffer, slots, fmt, SCALE)
+    size = buffer.shape[2]
+    roomy = torch.full((n, 1, size + 48), 255, dtype=torch.uint8, device="cuda")
+    roomy[..., :size] = buffer
+    wide = torch.full((n, 5, size), 255, dtype=torch.uint8, device="cuda")
+    wide[:, 3] = buffer[:, 0]
+    for held in (roomy[..., :size], wide[:, 3:4], buffer, buffer.as_strided((n, 1, size), (size, 16, 1))):
+        for got in _ways(binding, lambda: avsg.attend(q, held, slots, row_format=fmt, scale=SCALE, want_lse=True)):
+            ref.agree(*got, want)
