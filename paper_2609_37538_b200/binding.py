@@ -632,6 +632,20 @@ def _stream_of(stream, device: int) -> int:
     return _raw_stream(device)
 
 
+def _output(shape, dtype, device: int, stream: int):
+    """An output of a call on that stream.  Its block is one of that stream's (another stream's may still be in use by what is queued
+    there), and when the tensor is dropped it waits for what the current stream has queued by then, which reads it."""
+    import torch
+    if stream == _stream_of(None, device):
+        return torch.empty(shape, dtype=dtype, device=device)
+    # (1: the handle that CUDA itself has for the default stream)
+    on = torch.cuda.ExternalStream(stream, device) if stream > 1 else torch.cuda.default_stream(device)
+    with torch.cuda.stream(on):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(torch.cuda.current_stream(device))
+    return out
+
+
 # The argument blocks, packed at once: a structure of ctypes filled field by field costs a microsecond for eight of them.
 _APPEND = struct.Struct("=4I3Q2Q2Q4QQ5Q")
 _ATTEND = struct.Struct("=6I5Q3QQ3QQ2f6Q")
@@ -672,8 +686,9 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     latent [n, n_tokens, 512] and rope_part [n, n_tokens, 64]: CUDA tensors of one type (bf16, fp16, fp32), parts of a wider
     projection too; positions int32 [n, n_tokens], negative = padding; rows int32 like positions: where a token's row goes, if
     not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
-    table, as avsg_step takes them (without kv_rows a tensor's own bytes are the limit, an address has none); a tensor [rows, bytes] is a pool that all tables share.  Returns the values tensor (bf16 [n,
-    n_tokens, 576], what the rows stand for) where one is wanted, else None."""
+    table, as avsg_step takes them (without kv_rows a tensor's own bytes are the limit, an address has none); a tensor [rows, bytes] is a pool
+    that all tables share.  stream: a torch stream or a handle (default: the current one of latent's device).  Returns the values tensor (bf16
+    [n, n_tokens, 576], what the rows stand for; allocated on that stream) where one is wanted, else None."""
     import torch
     if _append_fn is None:
         _rows_functions()
@@ -694,6 +709,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
             rope_part.stride(2) != 1:
         raise AvsgError(EINVAL, "append: rope_part is a tensor [n, n_tokens, 64] of latent's type (bf16, fp16, fp32) and device, with its last "
                                 "numbers side by side")
+    stream = _stream_of(stream, device)
     size = 4 if kind == 2 else 2
     here = (n, n_tokens)
     kv_base = at = table_step = 0
@@ -723,7 +739,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     limits, limits_at = _c_array("I", kv_rows, n)
     tables, tables_at = _c_array("I", _tables, n)
     if want_values and values is None:
-        values = torch.empty((n, n_tokens, LATENT_DIMS + ROPE_DIMS), dtype=torch.bfloat16, device=latent.device)
+        values = _output((n, n_tokens, LATENT_DIMS + ROPE_DIMS), torch.bfloat16, device, stream)
     block = _APPEND.pack(
         n, n_tokens, row_format, kind, tables_at or 0, latent.data_ptr(), rope_part.data_ptr(), *_steps(latent, size, 2), *_steps(rope_part, size, 2),
         _tensor_at(positions, "append: positions", torch.int32, here, device),
@@ -731,7 +747,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
         0 if rope is None else rope.address,
         0 if values is None else _tensor_at(values, "append: values", torch.bfloat16, (n, n_tokens, LATENT_DIMS + ROPE_DIMS), device),
         0 if status is None else _addr(status))
-    rc = _append_fn(None if _ctx is None else _ctx._h, block, _stream_of(stream, device))
+    rc = _append_fn(None if _ctx is None else _ctx._h, block, stream)
     if rc != OK:
         _check(rc, "avsg_append")
     return values
@@ -744,7 +760,8 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     q: bf16 CUDA tensor [n, n_tokens, heads, 576]; buffer: uint8 [n, slots per table, row bytes] (avsg_step_noalloc's state;
     Context.attend reads the context's own); slots int32 [n, n_tokens, topk], negative = padding.  Optional: softcap; ids int32
     like slots with spans int32 [n, n_tokens, 2] (the ids [begin, end) that a query may see) and slopes fp32 [heads] with positions
-    int32 [n, n_tokens] (a bias of slope * (id - position)); rope with positions: q's last 64 numbers are rotated here.
+    int32 [n, n_tokens] (a bias of slope * (id - position)); rope with positions: q's last 64 numbers are rotated here.  stream: a torch stream
+    or a handle (default: the current one of q's device), on which outputs that are not given are allocated.
     Returns bf16 [n, n_tokens, heads, 512], and with want_lse the fp32 logarithms [n, n_tokens, heads] too."""
     import torch
     if _attend_fn is None:
@@ -760,6 +777,7 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     device, shape, bf16, int32 = q.get_device(), q.shape, torch.bfloat16, torch.int32
     if device < 0 or q.dtype is not bf16 or len(shape) != 4 or shape[3] != LATENT_DIMS + ROPE_DIMS or q.stride(3) != 1:
         raise AvsgError(EINVAL, "attend: q is a bf16 CUDA tensor [n, n_tokens, heads, 576] with its last numbers side by side")
+    stream = _stream_of(stream, device)
     n, n_tokens, heads, _ = shape
     _need(slots.dim() == 3, "attend: slots is [n, n_tokens, topk]")
     topk = slots.shape[2]
@@ -779,14 +797,14 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
         _need(len(_tables) == n, "attend: one table per block of queries")
         owner, tables_at = _c_array("I", _tables, n)
     if out is None:
-        out = torch.empty((n, n_tokens, heads, LATENT_DIMS), dtype=bf16, device=q.device)
+        out = _output((n, n_tokens, heads, LATENT_DIMS), bf16, device, stream)
         out_steps = (1024 * heads * n_tokens, 1024 * heads, 1024)
     else:
         if out.dtype is not bf16 or out.get_device() != device or out.shape != (n, n_tokens, heads, LATENT_DIMS) or out.stride(3) != 1:
             raise AvsgError(EINVAL, "attend: out is a bf16 tensor [n, n_tokens, heads, 512] on q's device with its last numbers side by side")
         out_steps = _steps(out, 2, 3)
     if want_lse and lse is None:
-        lse = torch.empty((n, n_tokens, heads), dtype=torch.float32, device=q.device)
+        lse = _output((n, n_tokens, heads), torch.float32, device, stream)
     block = _ATTEND.pack(
         n, n_tokens, topk, heads, row_format, rows, row_step, tables_at, rows_at, _tensor_at(slots, "attend: slots", int32, ids_like, device),
         q.data_ptr(), *_steps(q, 2, 3), out.data_ptr(), *out_steps,
@@ -796,7 +814,7 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
         0 if spans is None else _tensor_at(spans, "attend: spans", int32, (n, n_tokens, 2), device),
         0 if slopes is None else _tensor_at(slopes, "attend: slopes", torch.float32, (heads,), device),
         0 if rope is None else rope.address, 0 if status is None else _addr(status))
-    rc = _attend_fn(None if _ctx is None else _ctx._h, block, _stream_of(stream, device))
+    rc = _attend_fn(None if _ctx is None else _ctx._h, block, stream)
     if rc != OK:
         _check(rc, "avsg_attend")
     return out if lse is None else (out, lse)

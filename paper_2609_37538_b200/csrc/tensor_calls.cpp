@@ -6,6 +6,8 @@
 // places, a cache in one CUDA tensor.  Anything else answers NotImplemented, and the binding's own conversions decide what is
 // accepted and what is raised.
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -107,6 +109,24 @@ bool stream_of(PyObject* o, c10::DeviceIndex device, uint64_t* v)
     return true;
 }
 
+// An output of a call on that stream.  Its block is one of that stream's (another stream's may still be in use by what is queued
+// there), and when the tensor is dropped it waits for what the current stream has queued by then, which reads it.
+at::Tensor output(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like, uint64_t stream)
+{
+    const at::TensorOptions options = at::TensorOptions(type).device(like.device());
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(like.get_device());
+    if (reinterpret_cast<uint64_t>(current.stream()) == stream) return at::empty(shape, options);
+    at::Tensor t;
+    {
+        // (1: the handle that CUDA itself has for the default stream)
+        c10::cuda::CUDAStreamGuard guard(stream <= 1 ? c10::cuda::getDefaultCUDAStream(like.get_device())
+                                                     : c10::cuda::getStreamFromExternal(reinterpret_cast<cudaStream_t>(stream), like.get_device()));
+        t = at::empty(shape, options);
+    }
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+    return t;
+}
+
 // Answers (code, result): a code of avsg.h and the call's result.
 PyObject* answer(int rc, PyObject* result)
 {
@@ -171,12 +191,12 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         if (!o || o->get_device() != device || o->sizes() != at::IntArrayRef({n, T, H, (int64_t)AVSG_LATENT_DIMS})) return not_handled();
         out = *o;
     } else {
-        out = at::empty({n, T, H, (int64_t)AVSG_LATENT_DIMS}, at::TensorOptions(at::kBFloat16).device(q->device()));
+        out = output({n, T, H, (int64_t)AVSG_LATENT_DIMS}, at::kBFloat16, *q, stream);
     }
     s.out = out.data_ptr();
     steps(out, 3, s.out_stride);
     if (with_lse && !at) {
-        lse = at::empty({n, T, H}, at::TensorOptions(at::kFloat).device(q->device()));
+        lse = output({n, T, H}, at::kFloat, *q, stream);
         at = reinterpret_cast<uint64_t>(lse.data_ptr());
     }
     s.lse = reinterpret_cast<float*>(at);
@@ -254,7 +274,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     at::Tensor values;
     const bool made = !at && a[10] == Py_None && a[9] == Py_True;
     if (made) {
-        values = at::empty(at::IntArrayRef(wide, 3), at::TensorOptions(at::kBFloat16).device(latent->device()));
+        values = output(at::IntArrayRef(wide, 3), at::kBFloat16, *latent, stream);
         at = reinterpret_cast<uint64_t>(values.data_ptr());
     }
     s.values = reinterpret_cast<void*>(at);

@@ -53,3 +53,102 @@ def test_tables_of_one_row_with_room_behind_them(avsg, binding, fmt):           
     for held in (roomy[..., :size], wide[:, 3:4], buffer, buffer.as_strided((n, 1, size), (size, 16, 1))):
         for got in _ways(binding, lambda: avsg.attend(q, held, slots, row_format=fmt, scale=SCALE, want_lse=True)):
             ref.agree(*got, want)
+
+
+def _held_by_the_current_stream(like):
+    """A tensor of that shape and type, dropped while a copy of it is still to be made on the current stream; the copy, what it
+    has to hold, and the place of the dropped one."""
+    import torch
+    x = torch.empty_like(like)
+    x.fill_(3.0)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                       # about 0.1 s
+    return x.clone(), x.data_ptr()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("handle", [False, True], ids=["stream", "handle"])
+def test_outputs_of_a_call_on_another_stream(avsg, binding, fmt, handle):         # noqa: F811
+    # A block that was freed on the current stream may still be read by what is queued there: a call on another stream must not
+    # be given it.  And a result that is dropped while the current stream still has to read it is not written by the next call.
+    import torch
+    n, T, H, K, S = 16, 2, 128, 64, 128
+    q, buffer, slots = _problem(fmt, n, T, H, K, S, seed=82)
+    latent, part = q[..., 0, :512], q[..., 0, 512:]
+    positions = torch.arange(T, dtype=torch.int32, device="cuda").expand(n, T).contiguous()
+    many = torch.randn(4, 4096, 576, generator=_gen(83), device="cuda").to(torch.bfloat16)
+    at = torch.arange(4096, dtype=torch.int32, device="cuda").expand(4, 4096).contiguous()
+    cache = torch.zeros(4, 4096, buffer.shape[2], dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    on = side.cuda_stream if handle else side
+    calls = [lambda s: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, want_lse=True, stream=s)[0],
+             lambda s: avsg.append(many[..., :512], many[..., 512:], at, cache, row_format=fmt, want_values=True, stream=s)]
+    b, module = binding
+    for call in calls:
+        want = call(None).clone()
+        for way in (module, False):
+            b._tensor_calls = way
+            torch.cuda.synchronize()
+            torch.cuda.empty_cache()
+            kept, place = _held_by_the_current_stream(want)
+            out = call(on)
+            assert out.data_ptr() != place
+            side.synchronize()
+            torch.cuda.synchronize()
+            assert bool((kept == 3.0).all()), "a block that queued work still reads was written"
+            assert torch.equal(out, want)
+            # the result, read late by the current stream and dropped at once
+            torch.cuda.current_stream().wait_stream(side)
+            torch.cuda._sleep(200_000_000)
+            late = out.clone()
+            place = out.data_ptr()
+            del out
+            again = torch.empty_like(want).fill_(0)      # (of the current stream: may not be that block either)
+            out = call(on)
+            assert out.data_ptr() != place
+            with torch.cuda.stream(side):
+                out.fill_(5.0)
+            torch.cuda.synchronize()
+            assert torch.equal(late, want), "a result that queued work still reads was written"
+            del again
+        b._tensor_calls = module
+
+
+def test_a_call_on_the_default_stream_by_its_handle(avsg, binding):               # noqa: F811
+    # 0 and 1 (the legacy stream's own handle) name the default stream, also while another one is current
+    import torch
+    import rows_reference as ref
+    q, buffer, slots = _problem(1, 2, 1, 16, 64, 128, seed=84)
+    want = ref.attend(q, buffer, slots, 1, SCALE)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = [x for s in (0, 1) for x in _ways(binding, lambda: avsg.attend(q, buffer, slots, row_format=1, scale=SCALE, want_lse=True, stream=s))]
+    torch.cuda.synchronize()
+    for x in got:
+        ref.agree(*x, want)
+
+
+def test_outputs_of_a_captured_call_on_another_stream(avsg, binding):             # noqa: F811
+    # the call's stream joins a capture that another stream began
+    import torch
+    import rows_reference as ref
+    q, buffer, slots = _problem(1, 2, 1, 16, 64, 128, seed=85)
+    want = ref.attend(q, buffer, slots, 1, SCALE)
+    side = torch.cuda.Stream()
+    b, module = binding
+    for way in (module, False):
+        b._tensor_calls = way
+        avsg.attend(q, buffer, slots, row_format=1, scale=SCALE)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            side.wait_stream(torch.cuda.current_stream())
+            got = avsg.attend(q, buffer, slots, row_format=1, scale=SCALE, want_lse=True, stream=side)
+            torch.cuda.current_stream().wait_stream(side)
+        got[0].zero_()
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.agree(*got, want)
+    b._tensor_calls = module
