@@ -388,10 +388,12 @@ class Context:
         assert indices.is_cuda and indices.dtype == torch.int32 and indices.is_contiguous() and indices.dim() == 3
         n, n_q, K = indices.shape
         call = PreparedCall(self, table_ids, kv, n_q, K, row_stride, kv_rows)
-        slots = torch.empty_like(indices)
-        hit = torch.empty(indices.shape, dtype=torch.uint8, device=indices.device) if want_hit else None
-        mc = torch.empty((n, n_q), dtype=torch.int32, device=indices.device) if want_miss_count else None
-        arriving = torch.empty(indices.shape, dtype=torch.uint8, device=indices.device) if want_arriving else None
+        device = indices.get_device()
+        on = _stream_of(stream, device)
+        slots = _output(indices.shape, torch.int32, device, on)
+        hit = _output(indices.shape, torch.uint8, device, on) if want_hit else None
+        mc = _output((n, n_q), torch.int32, device, on) if want_miss_count else None
+        arriving = _output(indices.shape, torch.uint8, device, on) if want_arriving else None
         call.run(indices, verified_len, slots, hit, mc, stream, stage_one_done=stage_one_done, arriving=arriving)
         out = StepOutput(slots, hit, mc)
         out.arriving = arriving

@@ -152,3 +152,26 @@ def test_outputs_of_a_captured_call_on_another_stream(avsg, binding):           
         torch.cuda.synchronize()
         ref.agree(*got, want)
     b._tensor_calls = module
+
+
+def test_outputs_of_a_step_on_another_stream(avsg):                               # noqa: F811
+    # as above, for the slot table of Context.step
+    import torch
+    n, T, K, N = 4, 1, 2048, 4096
+    ctx = avsg.Context(num_tables=n, buffer_slots=4096, row_bytes=400, max_topk=K, max_tokens=T)
+    try:
+        kv = [torch.zeros(N, 400, dtype=torch.uint8, device="cuda") for _ in range(n)]
+        ids = torch.stack([torch.randperm(N, generator=_gen(86), device="cuda")[:K] for _ in range(n * T)]).to(torch.int32).view(n, T, K)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        kept, place = _held_by_the_current_stream(ids)
+        out = ctx.step([0, 1, 2, 3], ids, kv, [N] * n, stream=side)
+        assert place not in (out.slots.data_ptr(), out.hit.data_ptr(), out.miss_count.data_ptr())
+        torch.cuda.synchronize()
+        assert bool((kept == 3).all())
+        again = ctx.step([0, 1, 2, 3], ids, kv, [N] * n)
+        torch.cuda.synchronize()
+        assert torch.equal(out.slots, again.slots) and ctx.sync_status() == 0
+    finally:
+        ctx.close()
