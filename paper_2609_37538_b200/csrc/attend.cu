@@ -202,6 +202,17 @@ __device__ __forceinline__ void split(__half2 x, uint32_t& high, uint32_t& low)
     low = __nv_cvt_halfraw2_to_fp8x2(__half2_raw(__hsub2(x, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)high, __NV_E4M3)))), __NV_SATFINITE, __NV_E4M3);
 }
 
+// cap x tanh(x / cap) for a score in log2.  tanh(y) / y is a polynomial in y^2 where |y| < 0.6 (off by 2^-23 of itself; coefficients of the
+// least largest relative error, by reweighted least squares), so that a score far below its cap keeps its digits, and comes from exp2 beyond:
+// either is within 2^-20 of the result.  per_cap: 1 / cap in these units, in two factors, since the cap may be any number from 2^-126 on.
+__device__ __forceinline__ float capped(float x, float cap, const float (&per_cap)[2])
+{
+    const float y = x * per_cap[0] * per_cap[1], u = y * y;
+    const float near = x * (1.f + u * (-0.333325982f + u * (0.133131161f + u * (-0.0522118062f + u * 0.0156126339f))));
+    const float far = cap * (1.f - 2.f / (1.f + exp2f(y * (2.f * LOG2E)))) * LOG2E;
+    return fabsf(y) < 0.6f ? near : far;
+}
+
 __device__ __forceinline__ float logarithm(float most, float total) { return total == 0.f ? -INFINITY : (most + log2f(total)) * 0.6931471805599453f; }
 
 // The sums of a cluster's C blocks, joined: a warp takes a head, or half or a quarter of one, tasks going to the blocks in turn; lanes 0 .. C - 1
@@ -523,8 +534,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             if (k == 1 && !two) continue;
-                            // cap x tanh(x / cap), by exp2 alone: off by 2^-22 of the cap at most, however small x is
-                            if (p.softcap > 0.f) x[k][c] = p.softcap * LOG2E * (1.f - 2.f / (1.f + exp2f(x[k][c] * (2.f / p.softcap))));
+                            if (p.softcap > 0.f) x[k][c] = capped(x[k][c], p.softcap, p.per_cap);
                             if (p.slopes) x[k][c] += slope[k] * away;
                         }
                     }

@@ -145,6 +145,9 @@ int attend_run(const avsg_attend_args* a, const void* buffer, uint32_t rows, uin
     p.slopes = a->slopes; p.status = status;
     for (int i = 0; i < 3; ++i) { p.q_stride[i] = a->q_stride[i]; p.out_stride[i] = a->out_stride[i]; }
     p.scale = a->scale; p.softcap = a->softcap;
+    // (either factor, and a score times the first, stays within the range of normal floats for every cap)
+    p.per_cap[0] = a->softcap >= 1.f ? 5.9604644775390625e-8f : 1.f;                        // 2^-24
+    p.per_cap[1] = a->softcap > 0.f ? (float)(0.69314718055994530942 / a->softcap / p.per_cap[0]) : 0.f;
     p.n_tokens = a->n_tokens; p.topk = a->topk; p.heads = a->heads;
     p.rope = rope_params(a->rope);
     p.mapped = a->table_ids != nullptr;

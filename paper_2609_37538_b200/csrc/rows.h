@@ -48,7 +48,7 @@ struct AttendParams {
     const uint8_t* q; uint64_t q_stride[3];
     uint8_t* out; uint64_t out_stride[3];
     float* lse; uint32_t* status;
-    float scale, softcap;
+    float scale, softcap, per_cap[2];           // 1 / (softcap log2(e)) is per_cap[0] x per_cap[1]
     uint32_t n, n_tokens, topk, heads;
     uint32_t groups, group_heads, cluster;      // set by launch_attend(): groups of heads, heads of one, blocks per query and group
     RopeParams rope;

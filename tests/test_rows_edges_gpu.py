@@ -175,3 +175,43 @@ def test_outputs_of_a_step_on_another_stream(avsg):                             
         assert torch.equal(out.slots, again.slots) and ctx.sync_status() == 0
     finally:
         ctx.close()
+
+
+CAPS = [2.0 ** -126, 1e-30, 0.5, 3.0, 15.0, 50.0, 1e3, 1e5, 1e7, 1e10, 2.0 ** 100, 2.0 ** 126, 3.4028234e38]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("size", [1e-3, 1.0, 300.0])
+def test_capped_scores_keep_their_digits_under_any_cap(avsg, fmt, size):          # noqa: F811
+    """One row to a query: lse is its score.  The same call without a cap gives the score z that goes into the cap.
+
+    The bound.  |z| / cap < 0.6: tanh(y) / y as a polynomial, off by 2^-23 of itself, two more roundings.  Else 1 - 2 / (1 + exp2(.)): the
+    argument is off by 5 x 2^-24 of itself (scale, cap and constant rounded, two products), which moves tanh by y sech(y)^2 of that, 2.1 x
+    2^-24 at most; exp2 is off by 2^-22.5, of which sech(y)^2 / 2 <= 0.36 arrives; the quotient by 2^-22 of its 0.47 or less, the two sums by
+    2^-24 of 0.5 and 1: 6 x 2^-24 together where tanh is 0.54 or more, and three roundings of the product: 14 x 2^-24.  2^-20 covers both;
+    the two logarithms' own rounding is 4 x 2^-24.  Results below 2^-126 may count as zero."""
+    import torch
+    q, buffer, slots = _problem(fmt, 4, 4, 64, 1, 64, seed=87)
+    scale = SCALE * size
+    _, plain = avsg.attend(q, buffer, slots, row_format=fmt, scale=scale, want_lse=True)
+    z = plain.double()
+    assert z.abs().max() > size and (z.abs() < size).any()
+    for cap in CAPS:
+        out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=scale, want_lse=True, softcap=cap)
+        want = cap * torch.tanh(z / cap)
+        off = (lse.double() - want).abs()
+        allowed = want.abs() * (2.0 ** -20 + 2.0 ** -22) + 2.0 ** -124
+        assert bool((off <= allowed).all()), "cap %g: off by %.3g of %.3g allowed" % (cap, *(x[(off - allowed).argmax()].item() for x in (off.flatten(), allowed.flatten())))
+        assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("cap", [1e5, 1e8, 3.4028234e38])
+def test_attention_under_a_cap_far_above_its_scores(avsg, fmt, cap):              # noqa: F811
+    # cap x tanh(z / cap) is z to within z (z / cap)^2, far below a rounding: the bounds are those without a cap
+    import rows_reference as ref
+    q, buffer, slots = _problem(fmt, 2, 2, 24, 300, 512, seed=88)
+    out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, want_lse=True, softcap=cap)
+    _, _, eo, el = ref.attend(q, buffer, slots, fmt, SCALE)
+    want, want_lse, _, _ = ref.attend(q, buffer, slots, fmt, SCALE, softcap=cap)
+    ref.agree(out, lse, (want, want_lse, eo, el))
