@@ -59,7 +59,8 @@ __device__ __forceinline__ float2 sum_of_product(float2 a, float2 b, float2 c)
 
 // x / s such that a later rounding to few bits rounds the exact quotient: cut off towards zero, with the last bit set if anything was
 // cut (a quotient that is not a number of few bits is then none of their midpoints either).  r is 1 / s; q is within one step of the
-// quotient after one correction, and what is left, x - q s, says by its sign on which side of it.  (s is -scale here.)
+// quotient after one correction, and what is left, x - q s, says by its sign on which side of it.  (s is -scale here, 2^-40 or more in
+// magnitude: what is left of a quotient that matters, down to 2^-33 s, must not become zero.)
 __device__ __forceinline__ float2 sticky_quotients(float2 x, float2 s, float2 r)
 {
     float2 q = product(x, r);
@@ -148,12 +149,19 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
         if constexpr (FORMAT == AVSG_ROW_FP8) {
             const float scale = most >= 0x7F800000u ? __uint_as_float(most)
                                                     : fmaxf(__fdiv_rn(__uint_as_float(most), 448.f), 1.17549435e-38f);
-            const float inverse = __frcp_rn(scale);
+            // Where the group is tiny, numbers and scale go up by the same power of two, which leaves the quotients as they are.
+            float divisor = scale;
+            if (scale < 9.09494701772928237915e-13f) {                            // 2^-40
+                divisor *= 18446744073709551616.f;                                // 2^64
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] *= 18446744073709551616.f;
+            }
+            const float inverse = __frcp_rn(divisor);
             uint4 code;
             __nv_fp8x2_storage_t* c = reinterpret_cast<__nv_fp8x2_storage_t*>(&code);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                c[i] = __nv_cvt_float2_to_fp8x2(sticky_quotients(make_float2(x[2 * i], x[2 * i + 1]), make_float2(-scale, -scale), make_float2(inverse, inverse)),
+                c[i] = __nv_cvt_float2_to_fp8x2(sticky_quotients(make_float2(x[2 * i], x[2 * i + 1]), make_float2(-divisor, -divisor), make_float2(inverse, inverse)),
                                                 __NV_SATFINITE, __NV_E4M3);
             reinterpret_cast<uint4*>(out)[lane] = code;
             if (lane % LANES == 0) reinterpret_cast<float*>(out + LATENT)[lane / LANES] = scale;

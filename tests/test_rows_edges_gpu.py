@@ -215,3 +215,24 @@ def test_attention_under_a_cap_far_above_its_scores(avsg, fmt, cap):            
     _, _, eo, el = ref.attend(q, buffer, slots, fmt, SCALE)
     want, want_lse, _, _ = ref.attend(q, buffer, slots, fmt, SCALE, softcap=cap)
     ref.agree(out, lse, (want, want_lse, eo, el))
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_append_of_tiny_groups(avsg, fmt, dtype):                                 # noqa: F811
+    # groups down to where magnitudes count as zero (2^-126): codes are still the nearest to number / scale itself
+    import torch
+    import rows_reference as ref
+    T = 400
+    g = _gen(89)
+    size = torch.exp2(-90.0 - 36.0 * torch.arange(T, device="cuda", dtype=torch.float64) / T)[:, None]
+    x = torch.randn(T, 512, generator=g, device="cuda", dtype=torch.float64) * size
+    x[::2, 1::2] = torch.round(x[::2, 1::2] / size[::2] * 16) / 16 * size[::2]     # (few bits: next to ties, or on them)
+    x = x.to(getattr(torch, dtype))
+    x = torch.where(x.double().abs() < 2.0 ** -126, torch.zeros_like(x), x)[None]
+    part = torch.zeros(1, T, 64, device="cuda", dtype=x.dtype)
+    positions = torch.arange(T, device="cuda", dtype=torch.int32)[None]
+    kv = torch.zeros(1, T, ref.BYTES[fmt], dtype=torch.uint8, device="cuda")
+    avsg.append(x, part, positions, kv, row_format=fmt)
+    want = ref.pack(x[0].double(), part[0].to(torch.bfloat16), fmt)
+    assert torch.equal(kv[0], want), "%d bytes differ" % int((kv[0] != want).sum())
