@@ -190,13 +190,13 @@ __global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_co
             word |= __shfl_down_sync(0xffffffffu, word, 1) << 8;
             word |= __shfl_down_sync(0xffffffffu, word, 2) << 16;
             if (lane < 16u && lane % 4u == 0) reinterpret_cast<uint32_t*>(out + LATENT / 2u)[lane / 4u] = word;
-            const float scale = odd ? __uint_as_float(0x7FC00000u) : ldexpf(1.f, e);
+            const float twice = odd ? __uint_as_float(0x7FC00000u) : ldexpf(1.f, e + 1);       // (the scale itself may be 2^-127)
             if (values)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float2 v = __half22float2(e2m1_pair((i < 4 ? code.x : code.y) >> (i % 4 * 8) & 255u));
-                x[2 * i] = v.x * scale;
-                x[2 * i + 1] = v.y * scale;
+                x[2 * i] = 0.5f * v.x * twice;
+                x[2 * i + 1] = 0.5f * v.y * twice;
             }
         }
     }

@@ -236,3 +236,21 @@ def test_append_of_tiny_groups(avsg, fmt, dtype):                               
     avsg.append(x, part, positions, kv, row_format=fmt)
     want = ref.pack(x[0].double(), part[0].to(torch.bfloat16), fmt)
     assert torch.equal(kv[0], want), "%d bytes differ" % int((kv[0] != want).sum())
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_values_of_tiny_groups(avsg, fmt):                                        # noqa: F811
+    # what the rows stand for, down to 2^-126; the smallest scale of 4-bit rows, 2^-127, is below that itself
+    import torch
+    import rows_reference as ref
+    T = 64
+    x = torch.randn(T, 512, generator=_gen(93), device="cuda") * torch.exp2(-118.0 - 9.0 * torch.arange(T, device="cuda") / T)[:, None]
+    x = torch.where(x.abs() < 2.0 ** -126, torch.zeros_like(x), x)[None]
+    part = torch.zeros(1, T, 64, device="cuda")
+    positions = torch.arange(T, device="cuda", dtype=torch.int32)[None]
+    kv = torch.zeros(1, T, ref.BYTES[fmt], dtype=torch.uint8, device="cuda")
+    values = avsg.append(x, part, positions, kv, row_format=fmt, want_values=True)[0].double()
+    assert torch.equal(kv[0], ref.pack(x[0].double(), part[0].to(torch.bfloat16), fmt))
+    stands = ref.unpack(kv[0], fmt).float().to(torch.bfloat16).double()
+    small = stands.abs() < 2.0 ** -126
+    assert torch.equal(values[~small], stands[~small]) and bool((values[small].abs() < 2.0 ** -126).all()) and bool(small.any()) and bool((~small).any())
