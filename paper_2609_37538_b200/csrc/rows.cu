@@ -36,6 +36,15 @@ int device_of(const void* p, int* device)
 
 namespace {
 
+// The kernels write to a caller's status word only when something is wrong: where it lies is looked at in every call.
+int check_status(const uint32_t* status, int device)
+{
+    int at = -1;
+    if (!status) return AVSG_OK;
+    const int rc = device_of(status, &at);
+    return rc != AVSG_OK ? rc : at == device ? AVSG_OK : AVSG_EINVAL;
+}
+
 // Makes `device` current; its kernels are loaded by the first call on it.
 struct OnDevice {
     int prev = -1, rc = AVSG_OK;
@@ -173,7 +182,7 @@ int append_bare(const avsg_append_args* a, cudaStream_t stream)
     int rc = check_append(a), device = -1;
     if (rc != AVSG_OK) return rc;
     if (a->table_ids) return AVSG_EINVAL;
-    if ((rc = device_of(a->positions, &device)) != AVSG_OK) return rc;
+    if ((rc = device_of(a->positions, &device)) != AVSG_OK || (rc = check_status(a->status, device)) != AVSG_OK) return rc;
     OnDevice on(device);
     if (on.rc != AVSG_OK) return on.rc;
     return append_run(a, a->status, stream);
@@ -186,7 +195,7 @@ int attend_bare(const avsg_attend_args* a, cudaStream_t stream)
     const uint64_t bytes = row_bytes_of(a->row_format), stride = a->buffer_row_bytes ? a->buffer_row_bytes : bytes;
     if (a->table_ids || !a->buffer || !aligned(a->buffer, 16) || a->buffer_slots == 0 || a->buffer_slots > 0x80000000u) return AVSG_EINVAL;
     if (stride % 16 || stride < bytes || stride > 0xFFFFFFFFull) return AVSG_EINVAL;
-    if ((rc = device_of(a->slots, &device)) != AVSG_OK) return rc;
+    if ((rc = device_of(a->slots, &device)) != AVSG_OK || (rc = check_status(a->status, device)) != AVSG_OK) return rc;
     OnDevice on(device);
     if (on.rc != AVSG_OK) return on.rc;
     return attend_run(a, a->buffer, a->buffer_slots, stride, a->status, stream);

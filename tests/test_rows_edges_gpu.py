@@ -254,3 +254,14 @@ def test_values_of_tiny_groups(avsg, fmt):                                      
     stands = ref.unpack(kv[0], fmt).float().to(torch.bfloat16).double()
     small = stands.abs() < 2.0 ** -126
     assert torch.equal(values[~small], stands[~small]) and bool((values[small].abs() < 2.0 ** -126).all()) and bool(small.any()) and bool((~small).any())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_status_word_elsewhere_is_refused(avsg, binding, fmt):                  # noqa: F811
+    # (the calls have nothing to report)
+    import torch
+    q, buffer, slots = _problem(fmt, 2, 1, 4, 8, 32, seed=90)
+    positions = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    for status in (torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).pin_memory()):
+        _refused(avsg, binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, status=status))
+        _refused(avsg, binding, lambda: avsg.append(q[..., 0, :512], q[..., 0, 512:], positions, buffer, row_format=fmt, status=status))
