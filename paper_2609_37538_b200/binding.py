@@ -675,10 +675,32 @@ def _stream_number(stream):
     return stream if stream is None or type(stream) is int else _stream_handle(stream) or 0
 
 
-def _rows_in(kv, bytes_: int, stride) -> int:
-    """Rows that a cache given as a tensor has room for."""
-    span = (sum((size - 1) * step for size, step in zip(kv.shape, kv.stride())) + 1) * kv.element_size() if kv.numel() else 0
+def _rows_in(kv, bytes_: int, stride):
+    """Rows that a cache given as a tensor (a HostKV range, a packed array) has room for; None: an address."""
+    if hasattr(kv, "element_size"):
+        if kv.is_contiguous():
+            span = kv.nbytes
+            if stride is None:
+                return min(span // bytes_, 0x80000000)
+        else:
+            span = (sum((size - 1) * step for size, step in zip(kv.shape, kv.stride())) + 1) * kv.element_size() if kv.numel() else 0
+    elif isinstance(kv, HostKV) or (isinstance(kv, np.ndarray) and kv.flags.c_contiguous):
+        span = kv.nbytes
+    else:
+        return None
     return 0 if span < bytes_ else min((span - bytes_) // (stride or bytes_) + 1, 0x80000000)
+
+
+def _limits(most, kv_rows):
+    """Rows of each cache: `most` (None: no limit known), or fewer where the caller says so."""
+    if kv_rows is None:
+        return None if all(m is None for m in most) else [0x80000000 if m is None else m for m in most]
+    kv_rows = list(kv_rows)
+    _need(len(kv_rows) == len(most), "append: one kv_rows per table")
+    for m, r in zip(most, kv_rows):
+        if m is not None and r > m:
+            raise AvsgError(EINVAL, "append: kv_rows says %s rows, the cache has room for %s" % (r, m))
+    return kv_rows
 
 
 def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[Rope] = None, rows=None, row_stride=None, kv_rows=None,
@@ -688,8 +710,8 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     latent [n, n_tokens, 512] and rope_part [n, n_tokens, 64]: CUDA tensors of one type (bf16, fp16, fp32), parts of a wider
     projection too; positions int32 [n, n_tokens], negative = padding; rows int32 like positions: where a token's row goes, if
     not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
-    table, as avsg_step takes them (without kv_rows a tensor's own bytes are the limit, an address has none); a tensor [rows, bytes] is a pool
-    that all tables share.  stream: a torch stream or a handle (default: the current one of latent's device).  Returns the values tensor (bf16
+    table, as avsg_step takes them (a tensor's own bytes are the limit, kv_rows may set a lower one; an address has none but
+    kv_rows); a tensor [rows, bytes] is a pool that all tables share.  stream: a torch stream or a handle (default: the current one of latent's device).  Returns the values tensor (bf16
     [n, n_tokens, 576], what the rows stand for; allocated on that stream) where one is wanted, else None."""
     import torch
     if _append_fn is None:
@@ -725,8 +747,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
                                     "list of caches")
         _need(row_stride is None, "append: row_stride goes with a list of caches")
         at, table_step = kv.data_ptr(), (kv.stride(0) if len(full) == 3 and n > 1 else 0)
-        if kv_rows is None:
-            kv_rows = [full[-2]] * n
+        kv_rows = _limits([full[-2]] * n, kv_rows)
         if full[-2] > 1 and kv.stride(-2) != bytes_:
             row_stride = [kv.stride(-2)] * n
     else:
@@ -734,9 +755,11 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
         _need(len(kv) == n, "append: one cache per table")
         owner, kv_base = _c_array("Q", [_addr(k) for k in kv], n)
         keep.append(owner)
-        if kv_rows is None and all(hasattr(k, "stride") and hasattr(k, "element_size") for k in kv):
-            # a tensor's own bytes are the cache's limit
-            kv_rows = [_rows_in(k, row_bytes(row_format), None if row_stride is None else row_stride[i]) for i, k in enumerate(kv)]
+        if row_stride is not None:
+            row_stride = list(row_stride)
+            _need(len(row_stride) == n, "append: one row_stride per table")
+        # a tensor's own bytes are the cache's limit; an address has none
+        kv_rows = _limits([_rows_in(k, row_bytes(row_format), None if row_stride is None else row_stride[i]) for i, k in enumerate(kv)], kv_rows)
     strides, strides_at = _c_array("Q", row_stride, n)
     limits, limits_at = _c_array("I", kv_rows, n)
     tables, tables_at = _c_array("I", _tables, n)

@@ -265,3 +265,36 @@ def test_a_status_word_elsewhere_is_refused(avsg, binding, fmt):                
     for status in (torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).pin_memory()):
         _refused(avsg, binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, status=status))
         _refused(avsg, binding, lambda: avsg.append(q[..., 0, :512], q[..., 0, 512:], positions, buffer, row_format=fmt, status=status))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_more_rows_than_a_cache_tensor_has_are_refused(avsg, binding, fmt):       # noqa: F811
+    # (the calls' positions lie within the tensors)
+    import torch
+    bytes_ = avsg.row_bytes(fmt)
+    n, R = 2, 6
+    latent, part = torch.ones(n, 1, 512, device="cuda"), torch.ones(n, 1, 64, device="cuda")
+    positions = torch.tensor([[5], [0]], dtype=torch.int32, device="cuda")
+    pool = torch.zeros(n, R, bytes_, dtype=torch.uint8, device="cuda")
+    apart = [torch.zeros(R * bytes_, dtype=torch.uint8, device="cuda") for _ in range(n)]
+    pinned = [avsg.pinned_empty(R * bytes_) for _ in range(n)]
+    huge = [avsg.pinned_empty(R * bytes_, huge_pages=True) for _ in range(n)]
+    for kv in (pool, pool[0], apart, pinned, huge, [apart[0].data_ptr(), pinned[0]]):
+        for rows in ([R, R + 1], [R], [R] * 3):
+            _refused(avsg, binding, lambda: avsg.append(latent, part, positions, kv, row_format=fmt, kv_rows=rows))
+        for got in _both(binding, lambda: avsg.append(latent, part, positions, kv, row_format=fmt, kv_rows=[R, R])):
+            assert got is None
+    # without kv_rows: what a table's own cache has no room for is reported, whatever the others are given as
+    late = torch.tensor([[5], [R]], dtype=torch.int32, device="cuda")
+    for kv in (pinned, huge, [apart[0].data_ptr(), apart[1]]):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        avsg.append(latent, part, late, kv, row_format=fmt, status=status)
+        assert int(status) == avsg.STATUS_BAD_ID
+    wide = [torch.zeros(R, bytes_ + 16, dtype=torch.uint8, device="cuda") for _ in range(n)]
+    _refused(avsg, binding, lambda: avsg.append(latent, part, positions, wide, row_format=fmt, row_stride=[bytes_ + 16] * n, kv_rows=[R + 1, R]))
+    _refused(avsg, binding, lambda: avsg.append(latent, part, positions, apart, row_format=fmt, row_stride=[bytes_]))
+    # addresses have no limit of their own
+    for got in _both(binding, lambda: avsg.append(latent, part, positions, [k.data_ptr() for k in apart], row_format=fmt, kv_rows=[R] * n)):
+        assert got is None
+    torch.cuda.synchronize()
+    assert all(k.view(R, bytes_)[p].any() for k, p in zip(apart, (5, 0)))
