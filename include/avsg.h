@@ -555,7 +555,7 @@ int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
  *
  * What is rounded: queries and rows are taken as they are (a rotated query to bf16); scores, their maxima and sums are of 32 bits (lse is good
  * to about 1e-5), and the cap, however far above a score, is applied to within 2^-20 of the capped score.  Weights become bf16 with AVSG_ROW_BF16, fp16 with the others, values of AVSG_ROW_FP8 fp16 as well (in units of the row's largest
- * scale); sums of values are of 32 bits, out is rounded to bf16.  With 8- and 4-bit rows each position's share is rounded to
+ * scale); sums of values are of 32 bits (with AVSG_ROW_BF16 they may overflow where topk times the largest value exceeds 2^112), out is rounded to bf16.  With 8- and 4-bit rows each position's share is rounded to
  * about 2^-22 of the largest numbers among the rows that the query sees (weighted or not), where the largest weight counts as 1, and what is below
  * 2^-100 may count as zero.  The same call on the same inputs gives the same bits.
  *

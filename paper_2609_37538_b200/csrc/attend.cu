@@ -79,9 +79,12 @@ constexpr uint32_t FULL = 0, FREE = 32, SUM_FULL = 48, SUM_FREE = 64, WEIGHTS = 
 constexpr uint32_t COL_OUT = 0, COL_S = 256, COLUMNS = 512;
 
 constexpr float LOG2E = 1.4426950408889634f;
-// The maximum that weights refer to lags behind by up to LAZY (log2), so that O is rescaled seldom (bf16 has the range for much more).  fp16
-// weights are whole to 2^-25 then, the largest being 1 to 2^15.  (2^4 to 2^15: 6% slower with scores that spread over 2^+-12.)
-template <uint32_t FORMAT> constexpr float LAZY = Layout<FORMAT>::HALF ? 15.f : 60.f;
+// The maximum that weights refer to lags behind by up to LAZY (log2), so that O is rescaled seldom.  fp16 weights are whole to 2^-25 then, the
+// largest being 1 to 2^15.  (2^4 to 2^15: 6% slower with scores that spread over 2^+-12.)  bf16 has the range for more, but O has to hold weights
+// times values: bf16 weights are in units of BF16_UNIT, the largest being 2^-15 to 2^15, so that 2048 values may be of 2^101.  (1 to 2^15: 3.5% slower
+// with one request; 1 to 2^60: 0.5% faster, but values of 2^95 overflowed.)
+template <uint32_t FORMAT> constexpr float LAZY = Layout<FORMAT>::HALF ? 15.f : 30.f;
+constexpr float BF16_UNIT = 32768.f;
 constexpr uint32_t LEAST_UNIT = 27u << 23;                  // 2^-100: no row's unit is smaller, so that ratios of units stay finite
 constexpr long long WAIT_CLOCKS = 1ll << 29;                // about 0.3 s: longer than any wait that ends
 
@@ -628,7 +631,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
                     for (int c = 0; c < COUNT / 2; ++c) {
                         const float v = exp2f(x[k][2 * c] - from), w = exp2f(x[k][2 * c + 1] - from);
                         total[k] += v + w;
-                        pair[k][c] = L::HALF ? bits(__floats2half2_rn(v, w)) : bf16_pair(v, w);
+                        pair[k][c] = L::HALF ? bits(__floats2half2_rn(v, w)) : bf16_pair(v * (1.f / BF16_UNIT), w * (1.f / BF16_UNIT));
                     }
                 }
             }
@@ -673,7 +676,7 @@ __global__ void __launch_bounds__(Layout<FORMAT>::THREADS, 1) avsg_attend_kernel
                 }
             }
         }
-        if (threadIdx.x == 0) misc->unit = L::HALF ? unit : 1.f;
+        if (threadIdx.x == 0) misc->unit = L::HALF ? unit : BF16_UNIT;
     } else if (warp < SOFTMAX_WARPS + ROW_WARPS) {
         // ---- rows ----
         // (lanes 0-7 speak for eight rows)

@@ -298,3 +298,24 @@ def test_more_rows_than_a_cache_tensor_has_are_refused(avsg, binding, fmt):     
         assert got is None
     torch.cuda.synchronize()
     assert all(k.view(R, bytes_)[p].any() for k, p in zip(apart, (5, 0)))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("size", [2.0 ** 40, 2.0 ** 95])
+def test_large_values_under_scores_that_rise(avsg, fmt, size):                    # noqa: F811
+    # Scores (of the rotated part alone) rise by 2^55 along the list, so that weights are taken against maxima of the past; what is
+    # summed up meanwhile must not leave the range of 32 bits.
+    import torch
+    import rows_reference as ref
+    K, H = 2048, 4
+    g = _gen(94)
+    x = torch.randn(K, 512, generator=g, device="cuda", dtype=torch.float64) * size
+    r = torch.zeros(K, 64, device="cuda", dtype=torch.bfloat16)
+    r[:, 0] = torch.arange(K, device="cuda") // 64 * 64.0
+    r[:, 1] = torch.arange(K, device="cuda") % 64
+    buffer = ref.pack(x, r, fmt)[None].contiguous()
+    q = torch.zeros(1, 1, H, 576, device="cuda", dtype=torch.bfloat16)
+    q[..., 512] = q[..., 513] = torch.tensor([1.0, 0.5, -1.0, 0.0], device="cuda", dtype=torch.bfloat16)
+    slots = torch.arange(K, device="cuda", dtype=torch.int32).view(1, 1, K)
+    out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=38.0 / K, want_lse=True)
+    ref.agree(out, lse, ref.attend(q, buffer, slots, fmt, 38.0 / K))
