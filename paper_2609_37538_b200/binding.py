@@ -651,6 +651,22 @@ def _output(shape, dtype, device: int, stream: int):
 # The argument blocks, packed at once: a structure of ctypes filled field by field costs a microsecond for eight of them.
 _APPEND = struct.Struct("=4I3Q2Q2Q4QQ5Q")
 _ATTEND = struct.Struct("=6I5Q3QQ3QQ2f6Q")
+
+
+def _packed(layout, what: str, *values) -> bytes:
+    try:
+        return layout.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise AvsgError(EINVAL, "%s: a number does not fit its argument (%s)" % (what, e)) from None
+
+
+def _status_word(status) -> int:
+    """Address of a word that status bits are added to."""
+    if hasattr(status, "element_size") and (status.element_size() != 4 or status.numel() == 0):
+        raise AvsgError(EINVAL, "status: a word of 32 bits on the call's device is expected, got %s %s" % (status.dtype, tuple(status.shape)))
+    return _addr(status)
+
+
 _ROWS_CALL = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p)
 _append_fn = _attend_fn = None
 _tensor_calls = False                                # the extension module that makes these calls (csrc/tensor_calls.cpp), where it loads
@@ -719,7 +735,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     if _tensor_calls and row_stride is None and kv_rows is None:
         done = _tensor_calls.append(
             None if _ctx is None else _ctx._h.value, _tables, latent, rope_part, positions, kv, row_format, None if rope is None else rope.address,
-            rows, bool(want_values), values, None if status is None else _addr(status), _stream_number(stream))
+            rows, bool(want_values), values, None if status is None else _status_word(status), _stream_number(stream))
         if done is not NotImplemented:
             if done[0] != OK:
                 _check(done[0], "avsg_append")
@@ -765,13 +781,14 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     tables, tables_at = _c_array("I", _tables, n)
     if want_values and values is None:
         values = _output((n, n_tokens, LATENT_DIMS + ROPE_DIMS), torch.bfloat16, device, stream)
-    block = _APPEND.pack(
+    block = _packed(
+        _APPEND, "append",
         n, n_tokens, row_format, kind, tables_at or 0, latent.data_ptr(), rope_part.data_ptr(), *_steps(latent, size, 2), *_steps(rope_part, size, 2),
         _tensor_at(positions, "append: positions", torch.int32, here, device),
         0 if rows is None else _tensor_at(rows, "append: rows", torch.int32, here, device), kv_base, at, table_step, strides_at or 0, limits_at or 0,
         0 if rope is None else rope.address,
         0 if values is None else _tensor_at(values, "append: values", torch.bfloat16, (n, n_tokens, LATENT_DIMS + ROPE_DIMS), device),
-        0 if status is None else _addr(status))
+        0 if status is None else _status_word(status))
     rc = _append_fn(None if _ctx is None else _ctx._h, block, stream)
     if rc != OK:
         _check(rc, "avsg_append")
@@ -794,7 +811,7 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     if _tensor_calls:
         done = _tensor_calls.attend(
             None if _ctx is None else _ctx._h.value, _tables, q, buffer, slots, row_format, scale, out, lse, bool(want_lse), softcap, ids,
-            positions, spans, slopes, None if rope is None else rope.address, None if status is None else _addr(status), _stream_number(stream))
+            positions, spans, slopes, None if rope is None else rope.address, None if status is None else _status_word(status), _stream_number(stream))
         if done is not NotImplemented:
             if done[0] != OK:
                 _check(done[0], "avsg_attend")
@@ -830,7 +847,8 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
         out_steps = _steps(out, 2, 3)
     if want_lse and lse is None:
         lse = _output((n, n_tokens, heads), torch.float32, device, stream)
-    block = _ATTEND.pack(
+    block = _packed(
+        _ATTEND, "attend",
         n, n_tokens, topk, heads, row_format, rows, row_step, tables_at, rows_at, _tensor_at(slots, "attend: slots", int32, ids_like, device),
         q.data_ptr(), *_steps(q, 2, 3), out.data_ptr(), *out_steps,
         0 if lse is None else _tensor_at(lse, "attend: lse", torch.float32, (n, n_tokens, heads), device), scale, softcap,
@@ -838,7 +856,7 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
         0 if positions is None else _tensor_at(positions, "attend: positions", int32, here, device),
         0 if spans is None else _tensor_at(spans, "attend: spans", int32, (n, n_tokens, 2), device),
         0 if slopes is None else _tensor_at(slopes, "attend: slopes", torch.float32, (heads,), device),
-        0 if rope is None else rope.address, 0 if status is None else _addr(status))
+        0 if rope is None else rope.address, 0 if status is None else _status_word(status))
     rc = _attend_fn(None if _ctx is None else _ctx._h, block, stream)
     if rc != OK:
         _check(rc, "avsg_attend")

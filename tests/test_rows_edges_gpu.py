@@ -319,3 +319,23 @@ def test_large_values_under_scores_that_rise(avsg, fmt, size):                  
     slots = torch.arange(K, device="cuda", dtype=torch.int32).view(1, 1, K)
     out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=38.0 / K, want_lse=True)
     ref.agree(out, lse, ref.attend(q, buffer, slots, fmt, 38.0 / K))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_numbers_and_status_words_that_do_not_fit_are_refused(avsg, binding, fmt):               # noqa: F811
+    import torch
+    q, buffer, slots = _problem(fmt, 2, 1, 4, 8, 32, seed=95)
+    latent, part, positions = q[..., 0, :512], q[..., 0, 512:], torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    for kw in (dict(scale=1e300), dict(scale=SCALE, softcap=1e39), dict(scale=SCALE, softcap=1 << 200)):
+        _refused(avsg, binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, **kw))
+    ctx = avsg.Context(num_tables=2, buffer_slots=32, row_bytes=avsg.row_bytes(fmt), max_topk=8)
+    try:
+        for wrong in (-1, 1 << 40):
+            _refused(avsg, binding, lambda: ctx.attend([0, 1], q, slots, row_format=wrong, scale=SCALE))
+            _refused(avsg, binding, lambda: avsg.append(latent, part, positions, [buffer[0], buffer[1]], row_format=wrong))
+    finally:
+        ctx.close()
+    for status in (torch.zeros(4, dtype=torch.uint8, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda"),
+                   torch.zeros(0, dtype=torch.int32, device="cuda")):
+        _refused(avsg, binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, status=status))
+        _refused(avsg, binding, lambda: avsg.append(latent, part, positions, buffer, row_format=fmt, status=status))
