@@ -553,11 +553,16 @@ int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
  * out = 0 and lse = -infinity.  Masked positions are not read, whatever their rows hold; a slot >= the rows of a table is
  * masked too and reported as AVSG_STATUS_BAD_SLOT.  A seen row that holds an infinity or a NaN may make all of its queries' outputs NaN.
  *
- * What is rounded: queries and rows are taken as they are (a rotated query to bf16); scores, their maxima and sums are of 32 bits (lse is good
- * to about 1e-5), and the cap, however far above a score, is applied to within 2^-20 of the capped score.  Weights become bf16 with AVSG_ROW_BF16, fp16 with the others, values of AVSG_ROW_FP8 fp16 as well (in units of the row's largest
- * scale); sums of values are of 32 bits (with AVSG_ROW_BF16 they may overflow where topk times the largest value exceeds 2^112), out is rounded to bf16.  With 8- and 4-bit rows each position's share is rounded to
- * about 2^-22 of the largest numbers among the rows that the query sees (weighted or not), where the largest weight counts as 1, and what is below
- * 2^-100 may count as zero.  The same call on the same inputs gives the same bits.
+ * What is rounded:
+ *   queries  are taken as they are (a rotated query to bf16), except with AVSG_ROW_FP8: there a head's latent numbers are the sum of two e4m3
+ *            numbers in units of its largest, exact down to 2^-9 of that and rounded to within 2^-17 of it below, so that one very large number
+ *            costs the small ones digits (scores are off by up to scale * 2^-17 * largest * the sum of those positions' |key|)
+ *   scores   and their maxima and sums are of 32 bits: lse is good to about 1e-5 where scores are of 20 or less and the above adds nothing.  The cap,
+ *            however far above a score, is applied to within 2^-20 of the capped score
+ *   weights  become bf16 with AVSG_ROW_BF16, fp16 with the others; values of AVSG_ROW_FP8 fp16 as well (in units of the row's largest scale)
+ *   sums     of values are of 32 bits (with AVSG_ROW_BF16 they may overflow where topk times the largest value exceeds 2^112), out is rounded to bf16
+ * With 8- and 4-bit rows each position's share is rounded to about 2^-22 of the largest numbers among the rows that the query sees (weighted or
+ * not), where the largest weight counts as 1, and what is below 2^-100 may count as zero.  The same call on the same inputs gives the same bits.
  *
  * The kernel's waits are bounded (about 0.3 s, far beyond any that ends): AVSG_STATUS_WAIT_TIMEOUT in the status word means that one of
  * them ran out, and that the call's outputs are not to be used.

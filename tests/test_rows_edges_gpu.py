@@ -339,3 +339,20 @@ def test_numbers_and_status_words_that_do_not_fit_are_refused(avsg, binding, fmt
                    torch.zeros(0, dtype=torch.int32, device="cuda")):
         _refused(avsg, binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, status=status))
         _refused(avsg, binding, lambda: avsg.append(latent, part, positions, buffer, row_format=fmt, status=status))
+
+
+@pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 10, 2.0 ** 12])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_queries_with_a_few_large_numbers(avsg, fmt, size):                       # noqa: F811
+    # Numbers below 2^-9 of a head's largest are rounded to 2^-17 of it with 8-bit rows, and with them only (the reference's bound has
+    # that term for this format alone).  Keys are small where the queries are large, so that it is the small numbers that decide.
+    import torch
+    import rows_reference as ref
+    q, buffer, slots = _problem(fmt, 2, 2, 20, 200, 256, seed=91)
+    x = ref.unpack(buffer.view(-1, buffer.shape[2]), fmt)
+    large = [3, 140, 300]
+    x[:, large] /= size
+    buffer = ref.pack(x[:, :512], x[:, 512:].to(torch.bfloat16), fmt).view(buffer.shape)
+    q[..., large] = (q[..., large].float() * size).to(torch.bfloat16)
+    out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, want_lse=True)
+    ref.agree(out, lse, ref.attend(q, buffer, slots, fmt, SCALE))
