@@ -592,7 +592,8 @@ typedef struct {
     float           softcap;        /* > 0 (2^-126 or more), or 0: none                                     */
     const int32_t  *ids;            /* DEVICE [n][n_tokens][topk]: the positions that the slots hold (indices of
                                        avsg_step); NULL unless spans or slopes are given                    */
-    const int32_t  *positions;      /* DEVICE [n][n_tokens]: the queries' positions; NULL unless slopes or rope are given */
+    const int32_t  *positions;      /* DEVICE [n][n_tokens]: the queries' positions; NULL unless slopes or rope are given
+                                       (with slopes, ids - position has to fit 32 bits)                     */
     const int32_t  *spans;          /* DEVICE [n][n_tokens][2] or NULL                                      */
     const float    *slopes;         /* DEVICE [heads] or NULL                                               */
     const avsg_rope *rope;          /* HOST, or NULL: the last 64 numbers of q come rotated; else they are rotated by

@@ -728,7 +728,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
     table, as avsg_step takes them (a tensor's own bytes are the limit, kv_rows may set a lower one; an address has none but
     kv_rows); a tensor [rows, bytes] is a pool that all tables share.  stream: a torch stream or a handle (default: the current one of latent's device).  Returns the values tensor (bf16
-    [n, n_tokens, 576], what the rows stand for; allocated on that stream) where one is wanted, else None."""
+    [n, n_tokens, 576], what the rows stand for; allocated on that stream; without a gradient) where one is wanted, else None."""
     import torch
     if _append_fn is None:
         _rows_functions()
@@ -804,7 +804,8 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
     like slots with spans int32 [n, n_tokens, 2] (the ids [begin, end) that a query may see) and slopes fp32 [heads] with positions
     int32 [n, n_tokens] (a bias of slope * (id - position)); rope with positions: q's last 64 numbers are rotated here.  stream: a torch stream
     or a handle (default: the current one of q's device), on which outputs that are not given are allocated.
-    Returns bf16 [n, n_tokens, heads, 512], and with want_lse the fp32 logarithms [n, n_tokens, heads] too."""
+    Returns bf16 [n, n_tokens, heads, 512], and with want_lse the fp32 logarithms [n, n_tokens, heads] too.  For serving: a result has no
+    gradient, also where q requires one."""
     import torch
     if _attend_fn is None:
         _rows_functions()
