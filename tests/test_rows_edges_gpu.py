@@ -356,3 +356,41 @@ def test_queries_with_a_few_large_numbers(avsg, fmt, size):                     
     q[..., large] = (q[..., large].float() * size).to(torch.bfloat16)
     out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, want_lse=True)
     ref.agree(out, lse, ref.attend(q, buffer, slots, fmt, SCALE))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_outputs_are_written_whole_and_nothing_beside_them(avsg, binding, fmt):   # noqa: F811
+    # the caller's outputs hold something else before each way; what a call allocates is kept while the other way runs
+    import torch
+    import rows_reference as ref
+    n, T, H, K = 2, 3, 20, 70
+    q, buffer, slots = _problem(fmt, n, T, H, K, 128, seed=92)
+    slots[1, 2] = -1
+    want = ref.attend(q, buffer, slots, fmt, SCALE)
+    b, module = binding
+    wide = torch.empty(n, T, H, 528, dtype=torch.bfloat16, device="cuda")
+    lses = torch.empty(3, n, T, H, device="cuda")
+    for way in (module, False):
+        b._tensor_calls = way
+        wide.fill_(float("nan"))
+        lses.fill_(float("nan"))
+        out, lse = avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, out=wide[..., 8:520], lse=lses[1])
+        ref.agree(out, lse, want)
+        assert wide[..., :8].isnan().all() and wide[..., 520:].isnan().all() and lses[::2].isnan().all()
+    b._tensor_calls = module
+    for got in _ways(binding, lambda: avsg.attend(q, buffer, slots, row_format=fmt, scale=SCALE, want_lse=True)):
+        ref.agree(*got, want)
+    latent, part = q[:, :, 0, :512], q[:, :, 0, 512:]
+    positions = torch.tensor([[0, 1, 2], [4, -1, 3]], dtype=torch.int32, device="cuda")
+    written = positions >= 0
+    stands = ref.unpack(ref.pack(latent.double().reshape(-1, 512), part.reshape(-1, 64), fmt), fmt).view(n, T, 576).float().to(torch.bfloat16)
+    values = torch.empty(3, n, T, 576, dtype=torch.bfloat16, device="cuda")
+    for way in (module, False):
+        b._tensor_calls = way
+        values.fill_(float("nan"))
+        kv = torch.full((n, 5, buffer.shape[2]), 17, dtype=torch.uint8, device="cuda")
+        assert avsg.append(latent, part, positions, kv, row_format=fmt, values=values[1]) is not None
+        assert torch.equal(values[1][written], stands[written]) and values[1][~written].isnan().all() and values[::2].isnan().all()
+    b._tensor_calls = module
+    for got in _ways(binding, lambda: avsg.append(latent, part, positions, kv, row_format=fmt, want_values=True)):
+        assert torch.equal(got[written], stands[written])
