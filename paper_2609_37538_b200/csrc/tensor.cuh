@@ -142,12 +142,6 @@ __device__ __forceinline__ uint32_t in_block(uint32_t at, uint32_t rank)       /
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float load_float(uint32_t at)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
-    return v;
-}
 __device__ __forceinline__ float4 load_float4(uint32_t at)
 {
     float4 v;
