@@ -734,7 +734,7 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
         _rows_functions()
     if _tensor_calls and row_stride is None and kv_rows is None:
         done = _tensor_calls.append(
-            None if _ctx is None else _ctx._h.value, _tables, latent, rope_part, positions, kv, row_format, None if rope is None else rope.address,
+            None if _ctx is None else _ctx._cell.value or None, _tables, latent, rope_part, positions, kv, row_format, None if rope is None else rope.address,
             rows, bool(want_values), values, None if status is None else _status_word(status), _stream_number(stream))
         if done is not NotImplemented:
             if done[0] != OK:
@@ -811,7 +811,7 @@ def attend(q, buffer, slots, *, row_format: int, scale: float, out=None, lse=Non
         _rows_functions()
     if _tensor_calls:
         done = _tensor_calls.attend(
-            None if _ctx is None else _ctx._h.value, _tables, q, buffer, slots, row_format, scale, out, lse, bool(want_lse), softcap, ids,
+            None if _ctx is None else _ctx._cell.value or None, _tables, q, buffer, slots, row_format, scale, out, lse, bool(want_lse), softcap, ids,
             positions, spans, slopes, None if rope is None else rope.address, None if status is None else _status_word(status), _stream_number(stream))
         if done is not NotImplemented:
             if done[0] != OK:

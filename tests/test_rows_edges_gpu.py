@@ -394,3 +394,13 @@ def test_outputs_are_written_whole_and_nothing_beside_them(avsg, binding, fmt): 
     b._tensor_calls = module
     for got in _ways(binding, lambda: avsg.append(latent, part, positions, kv, row_format=fmt, want_values=True)):
         assert torch.equal(got[written], stands[written])
+
+
+def test_calls_of_a_closed_context_are_refused(avsg, binding):                   # noqa: F811
+    import torch
+    q, buffer, slots = _problem(1, 2, 1, 4, 8, 32, seed=96)
+    ctx = avsg.Context(num_tables=2, buffer_slots=32, row_bytes=656, max_topk=8)
+    ctx.close()
+    positions = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    _refused(avsg, binding, lambda: ctx.attend([0, 1], q, slots, row_format=1, scale=SCALE))
+    _refused(avsg, binding, lambda: ctx.append([0, 1], q[..., 0, :512], q[..., 0, 512:], positions, buffer, row_format=1))
