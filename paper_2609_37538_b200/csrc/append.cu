@@ -93,8 +93,9 @@ __device__ __forceinline__ void put_values(uint8_t* to, uint32_t lane, const flo
 
 }  // namespace
 
+// (16 blocks an SM, 32 registers a thread, where the numbers come in 16 bits: 16.6 us for 32768 rows of e4m3 where 40 registers take 17.1)
 template <uint32_t FORMAT, uint32_t TYPE>
-__global__ void __launch_bounds__(WARPS * 32) avsg_append_kernel(const __grid_constant__ AppendParams p)
+__global__ void __launch_bounds__(WARPS * 32, TYPE == AVSG_TYPE_FP32 ? 12 : 16) avsg_append_kernel(const __grid_constant__ AppendParams p)
 {
     const uint32_t lane = threadIdx.x & 31u;
     const uint32_t at = blockIdx.x * WARPS + (threadIdx.x >> 5);
