@@ -2,9 +2,9 @@
 // in native code, since the host bounds the small calls.  Host time of a queued attend(), marshalled in Python / here:
 // 14.6 / 6.0 us, of an append() 9.6 / 3.9.
 //
-// Only what such calls usually carry is handled here: plain tensors (no subclass) of the documented types, shapes and
-// places, a cache in one CUDA tensor.  Anything else answers NotImplemented, and the binding's own conversions decide what is
-// accepted and what is raised.
+// Handled here: plain tensors (no subclass) of the documented types, shapes and places, and for append() a cache in one CUDA tensor
+// without row_stride or kv_rows.  Anything else answers NotImplemented, and the binding's own conversions decide what is accepted and
+// what is raised: a list of caches, as avsg_step takes them, and a cache in pinned memory too (52 us for an append() to 64 of them, 12 to one).
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
