@@ -559,7 +559,8 @@ int avsg_append(avsg_ctx *ctx, const avsg_append_args *args, void *cuda_stream);
  *            costs the small ones digits (scores are off by up to scale * 2^-17 * largest * the sum of those positions' |key|)
  *   scores   and their maxima and sums are of 32 bits: lse is good to about 1e-5 where scores are of 20 or less and the above adds nothing.  The cap,
  *            however far above a score, is applied to within 2^-20 of the capped score
- *   weights  become bf16 with AVSG_ROW_BF16, fp16 with the others; values of AVSG_ROW_FP8 fp16 as well (in units of the row's largest scale)
+ *   weights  become bf16 with AVSG_ROW_BF16 (below 2^-110 of the largest they may count as zero), fp16 with the others; values of AVSG_ROW_FP8
+ *            fp16 as well (in units of the row's largest scale)
  *   sums     of values are of 32 bits (with AVSG_ROW_BF16 they may overflow where topk times the largest value exceeds 2^112), out is rounded to bf16
  * With 8- and 4-bit rows each position's share is rounded to about 2^-22 of the largest numbers among the rows that the query sees (weighted or
  * not), where the largest weight counts as 1, and what is below 2^-100 may count as zero.  The same call on the same inputs gives the same bits.
