@@ -727,8 +727,9 @@ def append(latent, rope_part, positions, kv, *, row_format: int, rope: Optional[
     projection too; positions int32 [n, n_tokens], negative = padding; rows int32 like positions: where a token's row goes, if
     not to its position.  kv: a uint8 tensor [n, rows, bytes] (CUDA or pinned), or one pinned or CUDA tensor (or address) per
     table, as avsg_step takes them (a tensor's own bytes are the limit, kv_rows may set a lower one; an address has none but
-    kv_rows); a tensor [rows, bytes] is a pool that all tables share.  stream: a torch stream or a handle (default: the current one of latent's device).  Returns the values tensor (bf16
-    [n, n_tokens, 576], what the rows stand for; allocated on that stream; without a gradient) where one is wanted, else None."""
+    kv_rows); a tensor [rows, bytes] is a pool that all tables share.  stream: a torch stream or a handle (default: the current one of
+    latent's device).  Returns the values tensor (bf16 [n, n_tokens, 576], what the rows stand for; allocated on that stream; without a
+    gradient) where one is wanted, else None."""
     import torch
     if _append_fn is None:
         _rows_functions()
